@@ -17,6 +17,9 @@ Entry points mirror include/quick.h:
   (include/quick_grouped.h), ``pack_experts(experts)``
 * ``gemm_fused`` / ``grouped_gemm_fused`` with a bias and the gated SiLU
   (include/quick_fused.h), ``interleave_gate_up(gate, up)``
+* ``mxfp4_*``: microscaled 4-bit floating point (include/quick_mx.h, mx.py)
+* ``moe_route`` / ``moe_combine``: a mixture-of-experts layer's router and
+  the sum over a token's experts (include/quick_moe.h, moe.py)
 """
 from __future__ import annotations
 
@@ -166,6 +169,8 @@ def lib():
             L.quick_grouped_fused_workspace_bytes.restype = SZ
             L.quick_interleave_gate_up.argtypes = [P, P, P, P, P, P, I64, I64, I64, P, P, P]
             L.quick_interleave_gate_up.restype = I
+            mx._declare(L)
+            moe._declare(L)
             _lib = L
     return _lib
 
@@ -603,3 +608,12 @@ EXPORTED = (
     "quick_w4a16_grouped_gemm_fused",
     "quick_fused_workspace_bytes", "quick_grouped_fused_workspace_bytes", "quick_interleave_gate_up",
 )
+
+# the modules call this one's helpers, so they come last
+from . import moe, mx  # noqa: E402
+from .moe import (MAX_EXPERTS, MAX_GROUPS, MAX_TOPK, SCORE_SIGMOID, SCORE_SOFTMAX, Routing, moe_combine,  # noqa: E402
+                  moe_route, moe_route_workspace_bytes)
+from .mx import (MX_BLOCK, mxfp4_dequantize, mxfp4_gemm, mxfp4_grouped_gemm, mxfp4_linear,  # noqa: E402
+                 mxfp4_linear_workspace_bytes, mxfp4_pack, mxfp4_packed_sizes, mxfp4_quantize)
+
+EXPORTED += mx.EXPORTED + moe.EXPORTED

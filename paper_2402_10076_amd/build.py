@@ -2,7 +2,8 @@
 without a GPU).  quick_gemm.hip is compiled as five translation units in
 parallel (host code and the C ABI; the launches of the stream kernels, the
 tiled kernels, the wave-split kernel and its grouped form), then linked with
-the packing code."""
+the packing code, the microscaled 4-bit floating-point operators and those of
+mixture-of-experts layers."""
 from __future__ import annotations
 
 import os
@@ -26,7 +27,10 @@ UNITS = [("quick_pack.cpp", []),
          ("quick_gemm.hip", ["-DQUICK_PART=1"]),
          ("quick_gemm.hip", ["-DQUICK_PART=2"]),
          ("quick_gemm.hip", ["-DQUICK_PART=3"]),
-         ("quick_gemm.hip", ["-DQUICK_PART=4"])]
+         ("quick_gemm.hip", ["-DQUICK_PART=4"]),
+         ("quick_mx.hip", []),
+         ("quick_mx_gemm.hip", []),
+         ("quick_moe.hip", [])]
 
 
 def _msgs(r):
