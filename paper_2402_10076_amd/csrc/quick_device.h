@@ -44,7 +44,13 @@ __device__ __forceinline__ uint32_t ld8(rsrc_t r, uint32_t voff, uint32_t soff)
     return (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, voff, soff, 0);
 }
 
+// A value that is the same in every lane, kept in scalar registers.
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p)
+{
+    const uint64_t v = (uint64_t)p;
+    return (const uint8_t*)((uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v));
+}
 
 // 16-bit types in memory, by QUICK_F16 / QUICK_BF16.
 template <int DT>
