@@ -38,12 +38,11 @@ typedef struct quick_route {
     int group_best;      /* a group's score: the sum of its 1 or 2 best choices*/
     int renormalize;     /* nonzero: a token's weights are divided by their sum*/
     float scale;         /* factor of the weights                              */
-    const float* bias;   /* device, [E]: added to the scores for the choice
-                            only; NULL = none                                  */
 } quick_route_t;
 
 /* Experts and weights of every token, and the routed rows sorted by expert.
  *   logits   [T][E] of `dtype`, aligned to its element
+ *   bias     f32 [E], added to the scores for the choice alone; NULL = none
  *   s        softmax over the row, or sigmoid, in binary32.  A logit of -inf
  *            (an expert that is masked) has s = 0, also in a row that has
  *            nothing else; a NaN or +inf gives what the formula gives
@@ -63,9 +62,9 @@ typedef struct quick_route {
  * quick_moe_route_workspace_bytes() (0: may be NULL); calls that share one
  * must be ordered.
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, WORKSPACE, HIP. */
-int quick_moe_route(const void* logits, int dtype, int64_t T, int64_t E, const quick_route_t* route, int32_t* ids,
-                    float* weights, int32_t* offsets, int32_t* rows, int32_t* slots, void* workspace,
-                    size_t workspace_bytes, void* stream);
+int quick_moe_route(const void* logits, int dtype, int64_t T, int64_t E, const quick_route_t* route,
+                    const float* bias, int32_t* ids, float* weights, int32_t* offsets, int32_t* rows,
+                    int32_t* slots, void* workspace, size_t workspace_bytes, void* stream);
 size_t quick_moe_route_workspace_bytes(int64_t T, int64_t E, int64_t topk);
 
 /* out[t] = residual[t] + sum over j < topk of weights[t][j] * y[slots[t][j]].

@@ -15,9 +15,9 @@ constexpr int64_t kMaxGrid = (1 << 24) - 1;   // workgroups: a launch has under 
 
 // One thread per eight values, four neighbouring lanes per block: amax over
 // the eight, over the four lanes by two lane exchanges, then one 4-byte store
-// of codes and, from every fourth lane, the scale byte.  Nothing is computed
-// that is not also loaded once: bound by the bytes (2 or 4 in, 17/32 out per
-// value).
+// of codes and, from every fourth lane, the scale byte.  Bound by the bytes (2
+// or 4 in, 17/32 out per value); x is read past the caches (22016 x 4096 bf16
+// to codes and back: 72 us, 85 through them).
 // A row is `pieces` pieces of eight; a workgroup takes kUnroll * kThreads of
 // one row, with all loads issued before the first is used.
 template <int DT>
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const uint8_t* x,
         // lanes is inside or outside together
         const int64_t p = std::min(p0 + u * kThreads, pieces - 4 + (int64_t)(threadIdx.x & 3));
 #pragma unroll
-        for (int i = 0; i < NV; i++) raw[u][i] = *(const u4_t*)(xr + (p * NV + i) * 16);
+        for (int i = 0; i < NV; i++) raw[u][i] = __builtin_nontemporal_load((const u4_t*)(xr + (p * NV + i) * 16));
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; u++) {
@@ -59,7 +59,6 @@ template <int DT>
 __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(const uint32_t* codes, const uint8_t* scales,
                                                                  uint8_t* y, int64_t pieces)
 {
-    constexpr int NV = DT == QUICK_F32 ? 2 : 1;
     const int64_t p0 = (int64_t)blockIdx.x * (kUnroll * kThreads) + threadIdx.x;
     uint32_t c[kUnroll], s[kUnroll];
 #pragma unroll
@@ -90,7 +89,6 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(const uint32_t*
                                         to16x2<DT>(v[6], v[7])};
         }
     }
-    (void)NV;
 }
 
 // Source row of packed column n: with gate_up, tiles of 16 gate columns and

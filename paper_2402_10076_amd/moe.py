@@ -12,12 +12,13 @@ module.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple
 
 import torch
 
 import paper_2402_10076_amd as _q
-from paper_2402_10076_amd.mx import _TYPES, _TYPES16, _fail, _gpu, _type
+from paper_2402_10076_amd.mx import _TYPES, _TYPES16, _fail, _gpu, _plain, _type
 
 SCORE_SOFTMAX = 0
 SCORE_SIGMOID = 1
@@ -29,7 +30,7 @@ MAX_EXPERTS = 512
 class QuickRoute(ctypes.Structure):
     _fields_ = [("score", ctypes.c_int), ("topk", ctypes.c_int), ("groups", ctypes.c_int),
                 ("topk_groups", ctypes.c_int), ("group_best", ctypes.c_int), ("renormalize", ctypes.c_int),
-                ("scale", ctypes.c_float), ("bias", ctypes.c_void_p)]
+                ("scale", ctypes.c_float)]
 
 
 class Routing(NamedTuple):
@@ -44,13 +45,19 @@ class Routing(NamedTuple):
 
 def _declare(L):
     P, I64, SZ, I = ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_int
-    L.quick_moe_route.argtypes = [P, I, I64, I64, ctypes.POINTER(QuickRoute), P, P, P, P, P, P, SZ, P]
+    L.quick_moe_route.argtypes = [P, I, I64, I64, ctypes.POINTER(QuickRoute), P, P, P, P, P, P, P, SZ, P]
     L.quick_moe_route_workspace_bytes.argtypes = [I64, I64, I64]
     L.quick_moe_route_workspace_bytes.restype = SZ
     L.quick_moe_combine.argtypes = [P, I, I64, I64, P, P, I64, I64, P, P, P]
 
 
 EXPORTED = ("quick_moe_route", "quick_moe_route_workspace_bytes", "quick_moe_combine")
+
+
+@functools.lru_cache(maxsize=64)
+def _options(*fields):
+    """The C struct of a set of options (building it takes as long as a check of all arguments)."""
+    return QuickRoute(*fields)
 
 
 def moe_route_workspace_bytes(T: int, E: int, topk: int) -> int:
@@ -80,11 +87,9 @@ def moe_route(logits: torch.Tensor, topk: int, score: int = SCORE_SOFTMAX, bias:
         _q._dev(what, "bias", bias, logits, dtype=torch.float32, shape=(E,))
     if out is None:
         dev = logits.device
-        # one allocation for the integers: a small call is bound by the host
-        ints = torch.empty(3 * T * topk + E + 1, dtype=torch.int32, device=dev)
-        ids, slots, rows, offsets = ints.split((T * topk, T * topk, T * topk, E + 1))
-        out = Routing(ids.view(T, topk), torch.empty((T, topk), dtype=torch.float32, device=dev), offsets, rows,
-                      slots.view(T, topk))
+        ids = torch.empty((T, topk), dtype=torch.int32, device=dev)
+        out = Routing(ids, torch.empty((T, topk), dtype=torch.float32, device=dev), ids.new_empty(E + 1),
+                      ids.new_empty(T * topk), ids.new_empty((T, topk)))
     else:
         for name, shape in (("ids", (T, topk)), ("weights", (T, topk)), ("offsets", (E + 1,)), ("rows", (T * topk,)),
                             ("slots", (T, topk))):
@@ -101,9 +106,9 @@ def moe_route(logits: torch.Tensor, topk: int, score: int = SCORE_SOFTMAX, bias:
     else:
         _q._dev(what, "workspace", workspace, logits)
         wsb = workspace.nbytes
-    r = QuickRoute(score, topk, groups, topk_groups, group_best, int(bool(renormalize)), scale,
-                   bias.data_ptr() if bias is not None else None)
-    _q._check(L.quick_moe_route(logits.data_ptr(), dtype, T, E, ctypes.byref(r), out.ids.data_ptr(),
+    r = _options(score, topk, groups, topk_groups, group_best, int(bool(renormalize)), scale)
+    _q._check(L.quick_moe_route(logits.data_ptr(), dtype, T, E, ctypes.byref(r),
+                                bias.data_ptr() if bias is not None else None, out.ids.data_ptr(),
                                 out.weights.data_ptr(), out.offsets.data_ptr(), out.rows.data_ptr(),
                                 out.slots.data_ptr(), workspace.data_ptr() if wsb else None, wsb, hs),
               "quick_moe_route")
@@ -124,12 +129,14 @@ def moe_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, res
         _fail(_q.QUICK_ERR_INVALID_ARG, "%s: slots must be an int32 [T][topk] tensor", what)
     R, D = y.shape
     T, topk = slots.shape
-    _q._dev(what, "slots", slots, y, dtype=torch.int32)
-    _q._dev(what, "weights", weights, y, dtype=torch.float32, shape=(T, topk))
-    if residual is not None:
+    dev = y.get_device()
+    if not (_plain(slots, dev, torch.int32) and _plain(weights, dev, torch.float32) and weights.shape == slots.shape):
+        _q._dev(what, "slots", slots, y, dtype=torch.int32)
+        _q._dev(what, "weights", weights, y, dtype=torch.float32, shape=(T, topk))
+    if residual is not None and not (_plain(residual, dev, y.dtype) and residual.shape == (T, D)):
         _q._dev(what, "residual", residual, y, dtype=y.dtype, shape=(T, D))
     if out is None:
-        out = torch.empty((T, D), dtype=y.dtype, device=y.device)
+        out = y.new_empty((T, D))
     else:
         _q._dev(what, "out", out, y, dtype=y.dtype, shape=(T, D))
     _q._check(_q.lib().quick_moe_combine(y.data_ptr(), dtype, R, D, slots.data_ptr(), weights.data_ptr(), T, topk,

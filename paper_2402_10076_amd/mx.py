@@ -49,7 +49,16 @@ def _fail(status, text, *a):
     raise _q.QuickError(status, text % a)
 
 
+def _plain(t, device, dtype):
+    """Whether _dev has nothing to say against t, for the usual case (a small
+    call is bound by the host; _dev takes three times as long)."""
+    return (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.get_device() == device
+            and t.is_contiguous())
+
+
 def _gpu(what, name, t):
+    if type(t) is torch.Tensor and t.is_cuda:
+        return
     if not isinstance(t, torch.Tensor) or t.device.type != _q._DEVICE_TYPE:
         _fail(_q.QUICK_ERR_INVALID_ARG, "%s: %s must be a tensor on the GPU", what, name)
 
@@ -76,6 +85,8 @@ def _check_codes(what, codes, scales, ref=None):
         _fail(_q.QUICK_ERR_INVALID_ARG, "%s: codes must be on %s, not %s", what, ref.device, codes.device)
     K = codes.shape[-1] * 2
     _channels(what, K)
+    if _plain(scales, codes.get_device(), torch.uint8) and scales.shape == (*codes.shape[:-1], K // MX_BLOCK):
+        return K
     _q._dev(what, "scales", scales, codes, dtype=torch.uint8, shape=(*codes.shape[:-1], K // MX_BLOCK))
     return K
 
@@ -96,11 +107,11 @@ def mxfp4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: t
     if ldx < K:
         _fail(_q.QUICK_ERR_SHAPE, "%s: rows of x overlap (stride %d, K=%d)", what, ldx, K)
     if codes is None:
-        codes = torch.empty((rows, K // 2), dtype=torch.uint8, device=x.device)
+        codes = x.new_empty((rows, K // 2), dtype=torch.uint8)
     else:
         _q._dev(what, "codes", codes, x, dtype=torch.uint8, shape=(rows, K // 2))
     if scales is None:
-        scales = torch.empty((rows, K // MX_BLOCK), dtype=torch.uint8, device=x.device)
+        scales = x.new_empty((rows, K // MX_BLOCK), dtype=torch.uint8)
     else:
         _q._dev(what, "scales", scales, x, dtype=torch.uint8, shape=(rows, K // MX_BLOCK))
     _q._check(_q.lib().quick_mxfp4_quantize(x.data_ptr(), dtype, ldx, rows, K, codes.data_ptr(), scales.data_ptr(),
@@ -116,7 +127,7 @@ def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dty
     code = _type(what, "dtype", dtype, _TYPES)
     shape = (*codes.shape[:-1], K)
     if y is None:
-        y = torch.empty(shape, dtype=dtype, device=codes.device)
+        y = codes.new_empty(shape, dtype=dtype)
     else:
         _q._dev(what, "y", y, codes, dtype=dtype, shape=shape)
     _q._check(_q.lib().quick_mxfp4_dequantize(codes.data_ptr(), scales.data_ptr(), code,
@@ -178,7 +189,7 @@ def _out(what, y, ref, rows, N, activation, dtype):
             _fail(_q.QUICK_ERR_SHAPE, "%s: gated columns come in tiles of 32 (N=%d)", what, N)
         N //= 2
     if y is None:
-        return torch.empty((rows, N), dtype=dtype, device=ref.device)
+        return ref.new_empty((rows, N), dtype=dtype)
     _q._dev(what, "y", y, ref, dtype=dtype, shape=(rows, N))
     return y
 
@@ -240,7 +251,7 @@ def mxfp4_linear(x: torch.Tensor, packed: torch.Tensor, packed_scales: torch.Ten
     if workspace is None:
         wsb = L.quick_mxfp4_linear_workspace_bytes(M, N, K)
         if wsb:
-            workspace = torch.empty(wsb, dtype=torch.uint8, device=x.device)
+            workspace = x.new_empty(wsb, dtype=torch.uint8)
             if stream is not None:
                 workspace.record_stream(stream)
     else:

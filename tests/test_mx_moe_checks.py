@@ -238,10 +238,10 @@ def test_abi_moe():
 
     def route(x=A, dt=2, t=5, e=64, out=(A,) * 5, ws=A, wsb=1 << 30, **k):
         r = Q.moe.QuickRoute(k.get("score", 0), k.get("topk", 2), k.get("groups", 1), k.get("topk_groups", 1),
-                             k.get("group_best", 1), 1, 1.0, k.get("bias"))
-        return L.quick_moe_route(x, dt, t, e, ctypes.byref(r), *out, ws, wsb, None)
+                             k.get("group_best", 1), 1, 1.0)
+        return L.quick_moe_route(x, dt, t, e, ctypes.byref(r), k.get("bias"), *out, ws, wsb, None)
     assert route(dt=3) == route(score=2) == route(group_best=0) == route(group_best=3) == route(x=0) == ARG
-    assert L.quick_moe_route(A, 2, 5, 8, None, A, A, A, A, A, None, 0, None) == ARG
+    assert L.quick_moe_route(A, 2, 5, 8, None, None, A, A, A, A, A, None, 0, None) == ARG
     for i in range(5):
         out = [A] * 5
         out[i] = None
@@ -272,9 +272,9 @@ def test_headers_compile_as_plain_c(tmp_path):
     import subprocess
     src = tmp_path / "t.c"
     src.write_text('#include "quick_mx.h"\n#include "quick_moe.h"\nint main(void) {\n'
-                   "    size_t a, b;\n    quick_route_t r = {QUICK_SCORE_SIGMOID, 2, 1, 1, 1, 1, 1.0f, 0};\n"
+                   "    size_t a, b;\n    quick_route_t r = {QUICK_SCORE_SIGMOID, 2, 1, 1, 1, 1, 1.0f};\n"
                    "    if (quick_mxfp4_packed_sizes(32, 160, &a, &b) != QUICK_OK || a != 4096 || b != 512) return 1;\n"
-                   "    if (quick_moe_route(0, QUICK_F32, 4, 8, &r, 0, 0, 0, 0, 0, 0, 0, 0) != QUICK_ERR_INVALID_ARG) "
+                   "    if (quick_moe_route(0, QUICK_F32, 4, 8, &r, 0, 0, 0, 0, 0, 0, 0, 0, 0) != QUICK_ERR_INVALID_ARG) "
                    "return 2;\n    return QUICK_MAX_TOPK == 16 && QUICK_MAX_GROUPS == 64 ? 0 : 3;\n}\n")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     exe = str(tmp_path / "t")
