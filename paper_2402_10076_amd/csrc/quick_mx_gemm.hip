@@ -25,6 +25,9 @@ using namespace quick;
 
 typedef int i8_t __attribute__((ext_vector_type(8)));
 
+// The cache policy of a load of data that nothing reads again: non-temporal.
+constexpr int kOnce = 2;
+
 struct MxArgs {
     const uint8_t* codes;      // [T][K/2]
     const uint8_t* scales;     // [T][K/32]
@@ -164,9 +167,10 @@ __device__ __forceinline__ void barrier()
 // also across the end of a run; at the end of one the waves' sums are added up
 // through LDS in the order of the waves, by waves that take turns.
 // TAIL: K is not a multiple of 128; the blocks past its end are read as zero.
+// ONCE: the weights come past the caches.
 // XQ >= 0: activations x of that 16-bit type, at most kFusedRows rows; the
 // workgroup quantises them into LDS while its first weights are under way.
-template <int NT, int WK, int D, bool GRP, bool TAIL, int XQ>
+template <int NT, int WK, int D, bool GRP, bool TAIL, bool ONCE, int XQ>
 __global__ __launch_bounds__(64 * WK) void mx_stream_kernel(MxArgs a, int groups)
 {
     constexpr int BM = 16;
@@ -209,7 +213,8 @@ __global__ __launch_bounds__(64 * WK) void mx_stream_kernel(MxArgs a, int groups
         const rsrc_t rp = make_rsrc(ps + (int64_t)lg * NT * KQ * 256, in ? (uint32_t)tiles * KQ * 256 : 0);
 #pragma unroll
         for (int j = 0; j < NT; j++) {
-            w[d][j] = ld128(rw, (uint32_t)(j * KS) * 1024 + lane * 16, s * 1024);
+            w[d][j] = bits_as<u4_t>(__builtin_amdgcn_raw_buffer_load_b128(rw, (uint32_t)(j * KS) * 1024 + lane * 16, s * 1024,
+                                                                          ONCE ? kOnce : 0));
             ws[d][j] = ld32(rp, (uint32_t)(j * KQ) * 256 + lane * 4, (s >> 2) * 256);
         }
         if constexpr (XQ < 0) {
@@ -340,9 +345,10 @@ __device__ __forceinline__ f16_t mx_mfma32(u4_t a, u4_t b, f16_t c, uint32_t sa,
 
 // 16 bytes per lane from a buffer straight into LDS: lane l writes bytes
 // 16 l .. 16 l + 15 after the wave-uniform address dst.
+template <int AUX>
 __device__ __forceinline__ void dma16(rsrc_t r, void* dst, uint32_t voff, uint32_t soff)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)dst, 16, voff, soff, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)dst, 16, voff, soff, 0, AUX);
 }
 // A BM x BN tile of y by WM x WN waves of MB x NB blocks of 32 x 32, on the
 // 32x32x64 instruction (twice the flops of the 16x16x128 one per operand byte
@@ -355,8 +361,9 @@ __device__ __forceinline__ void dma16(rsrc_t r, void* dst, uint32_t voff, uint32
 //  * weights: one packed unit a copy, as it lies in memory.
 // The scales of four steps are copied together, into NS / 4 buffers.  Operands
 // are read from LDS half a step (64 channels) before they are multiplied.
+// ONCE: the weights come past the caches.
 // TAIL: K is not a multiple of 128.
-template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL>
+template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL, bool ONCE>
 __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel(MxArgs a, int row_tiles)
 {
     constexpr int W = WM * WN, MB = BM / WM / 32, NB = BN / WN / 32;
@@ -436,9 +443,9 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         const rsrc_t rx = make_rsrc(a.codes, s < KS ? xbytes : 0), rw = make_rsrc(pw, s < KS ? wbytes : 0);
 #pragma unroll
         for (int i = 0; i < IM; i++)
-            dma16(rx, st + min(i * W + wave, XC - 1) * 1024, !TAIL || s * 4 + piece < KB ? xo[i] : 0xFFFFFFF0u, s * 64);
+            dma16<0>(rx, st + min(i * W + wave, XC - 1) * 1024, !TAIL || s * 4 + piece < KB ? xo[i] : 0xFFFFFFF0u, s * 64);
 #pragma unroll
-        for (int i = 0; i < IN; i++) dma16(rw, st + BM * 64 + (i * W + wave) * 1024, wo[i], s * 1024);
+        for (int i = 0; i < IN; i++) dma16<ONCE ? kOnce : 0>(rw, st + BM * 64 + (i * W + wave) * 1024, wo[i], s * 1024);
     };
     // scales of four steps: a copy of 64 rows' 16 bytes each, and of four
     // weight tiles'; the last waves may repeat a copy
@@ -460,7 +467,7 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         for (int i = 0; i < CI; i++) {
             const int c = min(i * W + wave, CM + CN - 1);
             if (!TAIL || c >= CM)
-                dma16(make_rsrc(sbase[i], q < KQ ? sbytes[i] : 0), sc + c * 1024, so[i], q * sstep[i]);
+                dma16<0>(make_rsrc(sbase[i], q < KQ ? sbytes[i] : 0), sc + c * 1024, so[i], q * sstep[i]);
         }
     };
     // TAIL: a row's scales start anywhere, and past its end is the next row's:
@@ -704,10 +711,29 @@ constexpr int64_t kFusedValues = 57344;
 
 bool fused(int64_t M, int64_t K) { return M <= kFusedRows && M * K <= kFusedValues; }
 
+// Whether the weights come past the caches: where a tile of rows reads them
+// once, and they do not stay in the 256 MB cache from call to call anyway
+// (70B gate+up, 16 rows: 39.3 us, 42.5 through them; but 7B down, 23 MB and 16
+// rows, 10.5 against 8.0 where a call finds what the one before has left).
+constexpr int64_t kOnceBytes = (int64_t)192 << 20;
+
+bool weights_once(const MxArgs& a, double rows, int bm)
+{
+    return rows <= bm && (int64_t)std::min(a.E, a.M) * a.N * a.K / 2 >= kOnceBytes;
+}
+
+// f(std::true_type) or f(std::false_type).
+template <class F>
+void with_bool(bool b, F f)
+{
+    if (b) f(std::true_type{});
+    else f(std::false_type{});
+}
+
 // About 1536 workgroups (six for each compute unit), fewer where there are not
 // so many column tiles; each takes as many runs as that leaves.
 template <int NT, bool GRP>
-int launch_stream(const MxArgs& a, int xq, hipStream_t hs)
+int launch_stream(const MxArgs& a, double expert_rows, int xq, hipStream_t hs)
 {
     constexpr int WK = 8, D = NT == 4 ? 2 : 4;
     const int64_t rows = GRP ? a.M / 16 + std::min(a.E, a.M) : ceil_div(a.M, 16);
@@ -715,40 +741,41 @@ int launch_stream(const MxArgs& a, int xq, hipStream_t hs)
     const int64_t runs = ceil_div(ceil_div(a.N, 16), NT);
     const int groups = (int)ceil_div(runs, std::max<int64_t>(1, 1536 / rows));
     const dim3 grid((uint32_t)ceil_div(runs, groups), (uint32_t)rows), block(64 * WK);
-    if constexpr (!GRP && NT <= 2) {
-        if (xq >= 0) {
-            const size_t lds = (size_t)a.M * (a.K / 2 + a.K / 32);
-            if (xq == QUICK_F16) {
-                if (a.K % 128) mx_stream_kernel<NT, WK, D, false, true, QUICK_F16><<<grid, block, lds, hs>>>(a, groups);
-                else mx_stream_kernel<NT, WK, D, false, false, QUICK_F16><<<grid, block, lds, hs>>>(a, groups);
-            } else {
-                if (a.K % 128) mx_stream_kernel<NT, WK, D, false, true, QUICK_BF16><<<grid, block, lds, hs>>>(a, groups);
-                else mx_stream_kernel<NT, WK, D, false, false, QUICK_BF16><<<grid, block, lds, hs>>>(a, groups);
+    with_bool(a.K % 128 != 0, [&](auto tail) {
+        with_bool(weights_once(a, expert_rows, 16), [&](auto once) {
+            constexpr bool TAIL = decltype(tail)::value, ONCE = decltype(once)::value;
+            if constexpr (!GRP && NT <= 2) {
+                if (xq >= 0) {
+                    const size_t lds = (size_t)a.M * (a.K / 2 + a.K / 32);
+                    if (xq == QUICK_F16)
+                        mx_stream_kernel<NT, WK, D, false, TAIL, ONCE, QUICK_F16><<<grid, block, lds, hs>>>(a, groups);
+                    else
+                        mx_stream_kernel<NT, WK, D, false, TAIL, ONCE, QUICK_BF16><<<grid, block, lds, hs>>>(a, groups);
+                    return;
+                }
             }
-            return QUICK_OK;
-        }
-    }
-    if (a.K % 128) mx_stream_kernel<NT, WK, D, GRP, true, -1><<<grid, block, 0, hs>>>(a, groups);
-    else mx_stream_kernel<NT, WK, D, GRP, false, -1><<<grid, block, 0, hs>>>(a, groups);
+            mx_stream_kernel<NT, WK, D, GRP, TAIL, ONCE, -1><<<grid, block, 0, hs>>>(a, groups);
+        });
+    });
     return QUICK_OK;
 }
 
 template <int BM, int BN, int WM, int WN, int NS, bool GRP>
-int launch_tiled(const MxArgs& a, hipStream_t hs)
+int launch_tiled(const MxArgs& a, double expert_rows, hipStream_t hs)
 {
     const int64_t rows = GRP ? a.M / BM + std::min(a.E, a.M) : ceil_div(a.M, BM);
     const int64_t grid = ceil_div(rows * ceil_div(a.N, BN), 8) * 8;
     if (grid > (1 << 22)) return QUICK_ERR_SHAPE;
     const dim3 g((uint32_t)grid), block(64 * WM * WN);
-    if (a.K % 128) {
-        // not in the largest form: its accumulators leave no registers for it
-        if constexpr (BM * BN < 65536)
-            mx_tiled_kernel<BM, BN, WM, WN, NS, GRP, true><<<g, block, 0, hs>>>(a, (int)rows);
-        else
-            return QUICK_ERR_INVALID_ARG;
-    } else {
-        mx_tiled_kernel<BM, BN, WM, WN, NS, GRP, false><<<g, block, 0, hs>>>(a, (int)rows);
-    }
+    with_bool(a.K % 128 != 0, [&](auto tail) {
+        with_bool(weights_once(a, expert_rows, BM), [&](auto once) {
+            constexpr bool TAIL = decltype(tail)::value, ONCE = decltype(once)::value;
+            // no tail in the largest form: its accumulators leave no registers
+            // for it; and the tallest are for more rows than read weights once
+            if constexpr (!(TAIL && BM * BN >= 65536))
+                mx_tiled_kernel<BM, BN, WM, WN, NS, GRP, TAIL, ONCE && BM <= 64><<<g, block, 0, hs>>>(a, (int)rows);
+        });
+    });
     return QUICK_OK;
 }
 
@@ -818,20 +845,21 @@ template <bool GRP>
 int launch_mx(const MxArgs& a, int xq, hipStream_t hs)
 {
     const int64_t busy = GRP ? std::min(a.E, a.M) : 1;
-    const int form = choose_form((double)a.M / busy, busy, a.N, a.K, a.gated, xq >= 0);
+    const double rows = (double)a.M / busy;
+    const int form = choose_form(rows, busy, a.N, a.K, a.gated, xq >= 0);
     (void)hipGetLastError();
     int st = QUICK_OK;
     switch (form) {
-    case 0: st = launch_stream<1, GRP>(a, xq, hs); break;
-    case 1: st = launch_stream<2, GRP>(a, xq, hs); break;
-    case 2: st = launch_stream<4, GRP>(a, xq, hs); break;
-    case 3: st = launch_tiled<32, 128, 1, 4, 4, GRP>(a, hs); break;
-    case 4: st = launch_tiled<64, 64, 2, 2, 8, GRP>(a, hs); break;
-    case 5: st = launch_tiled<64, 128, 1, 4, 8, GRP>(a, hs); break;
-    case 6: st = launch_tiled<64, 128, 1, 4, 4, GRP>(a, hs); break;
-    case 7: st = launch_tiled<128, 128, 2, 2, 4, GRP>(a, hs); break;
-    case 8: st = launch_tiled<128, 256, 2, 4, 4, GRP>(a, hs); break;
-    default: st = launch_tiled<256, 256, 2, 4, 4, GRP>(a, hs); break;
+    case 0: st = launch_stream<1, GRP>(a, rows, xq, hs); break;
+    case 1: st = launch_stream<2, GRP>(a, rows, xq, hs); break;
+    case 2: st = launch_stream<4, GRP>(a, rows, xq, hs); break;
+    case 3: st = launch_tiled<32, 128, 1, 4, 4, GRP>(a, rows, hs); break;
+    case 4: st = launch_tiled<64, 64, 2, 2, 8, GRP>(a, rows, hs); break;
+    case 5: st = launch_tiled<64, 128, 1, 4, 8, GRP>(a, rows, hs); break;
+    case 6: st = launch_tiled<64, 128, 1, 4, 4, GRP>(a, rows, hs); break;
+    case 7: st = launch_tiled<128, 128, 2, 2, 4, GRP>(a, rows, hs); break;
+    case 8: st = launch_tiled<128, 256, 2, 4, 4, GRP>(a, rows, hs); break;
+    default: st = launch_tiled<256, 256, 2, 4, 4, GRP>(a, rows, hs); break;
     }
     return st ? st : launched();
 }
