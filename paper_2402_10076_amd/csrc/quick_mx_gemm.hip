@@ -370,6 +370,9 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     constexpr int XC = BM / 16, IM = (XC + W - 1) / W, IN = BN / 16 / W, NI = IM + IN;    // copies a wave and step
     constexpr int STAGE = (BM + BN) * 64, XS = BM < 64 ? 64 : BM, SC = (XS + BN) * 16;
     static_assert(IN * W * 16 == BN && (NS == 4 || NS == 8), "weight copies are shared out evenly");
+    // Operands go to registers a whole step before they are multiplied, but in
+    // the largest tile, whose accumulators leave room for half a step.
+    constexpr bool AHEAD = BM * BN < 65536;
     constexpr int S8 = NS == 8 ? STAGE : 16;
     __shared__ __attribute__((aligned(16))) uint8_t st0[STAGE], st1[STAGE], st2[STAGE], st3[STAGE], st4[S8], st5[S8],
         st6[S8], st7[S8], sc0[SC], sc1[NS == 8 ? SC : 16];
@@ -505,14 +508,15 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     const int wr = BM * 64 + (wn * NB * 2 + (col >> 4)) * 1024 + half * 256 + (col & 15) * 16;
     const int xsr = (wm * MB * 32 + col) * 16;
     const int wsr = XS * 16 + (wn * NB * 2 + (col >> 4)) * 256 + (half * 16 + (col & 15)) * 4;
-    u4_t x[2][MB], w[2][NB], xs[MB];
+    u4_t x[AHEAD ? 4 : 2][MB], w[AHEAD ? 4 : 2][NB], xs[MB];
     uint32_t ws[NB][2];
-    auto read = [&](const uint8_t* st, auto which) __attribute__((always_inline)) {
-        constexpr int h = decltype(which)::value;
+    // half step h of a step: AHEAD keeps two steps, the odd ones in 2 and 3
+    auto read = [&](const uint8_t* st, auto step, auto which) __attribute__((always_inline)) {
+        constexpr int h = decltype(which)::value, p = AHEAD ? decltype(step)::value % 2 * 2 + h : h;
 #pragma unroll
-        for (int j = 0; j < NB; j++) w[h][j] = *(const u4_t*)(st + wr + j * 2048 + h * 512);
+        for (int j = 0; j < NB; j++) w[p][j] = *(const u4_t*)(st + wr + j * 2048 + h * 512);
 #pragma unroll
-        for (int i = 0; i < MB; i++) x[h][i] = *(const u4_t*)(st + (xr ^ (h * 32)) + i * 2048);
+        for (int i = 0; i < MB; i++) x[p][i] = *(const u4_t*)(st + (xr ^ (h * 32)) + i * 2048);
     };
     // scales of steps 4 q ..: a row's byte of block 2 h + half of step j is
     // byte 2 h of word j here; zero for steps past the last one, which lie in
@@ -531,12 +535,12 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
             for (int h = 0; h < 2; h++) tw[j][h] = *(const uint32_t*)(sc + wsr + j * 512 + h * 128);
     };
     auto multiply = [&](auto step, auto which) __attribute__((always_inline)) {
-        constexpr int S = decltype(step)::value, h = decltype(which)::value;
+        constexpr int S = decltype(step)::value, h = decltype(which)::value, p = AHEAD ? S % 2 * 2 + h : h;
 #pragma unroll
         for (int i = 0; i < MB; i++)
 #pragma unroll
             for (int j = 0; j < NB; j++)
-                acc[i][j] = mx_mfma32<S, 2 * h>(w[h][j], x[h][i], acc[i][j], ws[j][h], xs[i][S]);
+                acc[i][j] = mx_mfma32<S, 2 * h>(w[p][j], x[p][i], acc[i][j], ws[j][h], xs[i][S]);
     };
 
     constexpr std::integral_constant<int, 0> I0;
@@ -558,11 +562,13 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         copy_step(st5, 5);
         copy_step(st6, 6);
     }
-    wait_vm<(NS - 2) * NI>();
+    if constexpr (AHEAD) copy_step(stage(std::integral_constant<int, NS - 1>{}), NS - 1);
+    wait_vm<(AHEAD ? NS - 1 : NS - 2) * NI>();
     wait_lds();
     barrier();
     read_scales(sc0, 0, xs, ws);
-    read(st0, I0);
+    read(st0, I0, I0);
+    if constexpr (AHEAD) read(st0, I0, I1);
     // Order of a half step: one matrix instruction, then some of the LDS reads
     // and copies that are issued under it.
     auto interleave = [&](auto reads, auto copies) __attribute__((always_inline)) {
@@ -579,30 +585,48 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     };
     // Step s.  After the barrier: the copies of step s + 1 have arrived (those
     // of later ones may be under way), and every wave has read all of step
-    // s - 1, whose stage is filled next.
+    // s - 1 (AHEAD: s), whose stage is filled next.
     auto turn = [&](int s, auto unrolled) __attribute__((always_inline)) {
         constexpr int U = decltype(unrolled)::value, S = U % 4;
-        wait_vm<(NS - 3) * NI>();
+        constexpr int FREED = AHEAD ? 0 : 1;      // the step after which scales are in registers
+        wait_vm<(AHEAD ? NS - 2 : NS - 3) * NI>();
         wait_lds();
         barrier();
         __builtin_amdgcn_sched_barrier(0);
         uint8_t* sc = scale_buffer(std::integral_constant<int, U / 4>{});
-        if constexpr (S == 1) {
+        if constexpr (S == FREED) {
             // the scales of this step's four are in registers
             load_tail(s / 4 + NS / 4);
             copy_scales(sc, s / 4 + NS / 4);
         }
         if constexpr (S == 2) write_tail(sc);
-        copy_step(stage(std::integral_constant<int, U + NS - 1>{}), s + NS - 1);
-        read(stage(std::integral_constant<int, U>{}), I1);
-        multiply(std::integral_constant<int, S>{}, I0);
-        interleave(std::integral_constant<int, MB + NB>{}, std::integral_constant<int, NI + (S == 1 ? CI : 0)>{});
+        constexpr std::integral_constant<int, U + 1> NEXT;
+        constexpr std::integral_constant<int, NI + (S == FREED ? CI : 0)> COPIES;
         u4_t nx[MB];
         uint32_t nw[NB][2];
-        if constexpr (S == 3) read_scales(scale_buffer(std::integral_constant<int, U / 4 + 1>{}), s / 4 + 1, nx, nw);
-        read(stage(std::integral_constant<int, U + 1>{}), I0);
-        multiply(std::integral_constant<int, S>{}, I1);
-        interleave(std::integral_constant<int, MB + NB + (S == 3 ? MB + 2 * NB : 0)>{}, I0);
+        auto next_scales = [&]() __attribute__((always_inline)) {
+            read_scales(scale_buffer(std::integral_constant<int, U / 4 + 1>{}), s / 4 + 1, nx, nw);
+        };
+        constexpr int SR = S == 3 ? MB + 2 * NB : 0;
+        if constexpr (AHEAD) {
+            copy_step(stage(unrolled), s + NS);
+            if constexpr (S == 3) next_scales();
+            read(stage(NEXT), NEXT, I0);
+            multiply(std::integral_constant<int, S>{}, I0);
+            interleave(std::integral_constant<int, MB + NB + SR>{}, COPIES);
+            read(stage(NEXT), NEXT, I1);
+            multiply(std::integral_constant<int, S>{}, I1);
+            interleave(std::integral_constant<int, MB + NB>{}, I0);
+        } else {
+            copy_step(stage(std::integral_constant<int, U + NS - 1>{}), s + NS - 1);
+            read(stage(unrolled), unrolled, I1);
+            multiply(std::integral_constant<int, S>{}, I0);
+            interleave(std::integral_constant<int, MB + NB>{}, COPIES);
+            if constexpr (S == 3) next_scales();
+            read(stage(NEXT), NEXT, I0);
+            multiply(std::integral_constant<int, S>{}, I1);
+            interleave(std::integral_constant<int, MB + NB + SR>{}, I0);
+        }
         if constexpr (S == 3) {
 #pragma unroll
             for (int i = 0; i < MB; i++) xs[i] = nx[i];
