@@ -374,8 +374,13 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     // the largest tile, whose accumulators leave room for half a step.
     constexpr bool AHEAD = BM * BN < 65536;
     constexpr int S8 = NS == 8 ? STAGE : 16;
-    __shared__ __attribute__((aligned(16))) uint8_t st0[STAGE], st1[STAGE], st2[STAGE], st3[STAGE], st4[S8], st5[S8],
-        st6[S8], st7[S8], sc0[SC], sc1[NS == 8 ? SC : 16];
+    // No more than eight objects, the number that the compiler tells apart in
+    // its waits: the scales lie behind the stages that are filled and read at
+    // the same turns
+    __shared__ __attribute__((aligned(16))) uint8_t st0[STAGE + SC], st1[STAGE], st2[STAGE], st3[STAGE],
+        st4[NS == 8 ? STAGE + SC : 16], st5[S8], st6[S8], st7[S8];
+    uint8_t* const sc0 = st0 + STAGE;
+    uint8_t* const sc1 = st4 + (NS == 8 ? STAGE : 0);
     auto scale_buffer = [&](auto which) __attribute__((always_inline)) -> uint8_t* {
         if constexpr (decltype(which)::value % (NS / 4) == 0) return sc0;
         else return sc1;
@@ -553,16 +558,10 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         write_tail(sc1);
         copy_scales(sc1, 1);
     }
-    copy_step(st0, 0);
-    copy_step(st1, 1);
-    copy_step(st2, 2);
-    if constexpr (NS == 8) {
-        copy_step(st3, 3);
-        copy_step(st4, 4);
-        copy_step(st5, 5);
-        copy_step(st6, 6);
-    }
-    if constexpr (AHEAD) copy_step(stage(std::integral_constant<int, NS - 1>{}), NS - 1);
+    auto first_copies = [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
+        ((copy_step(stage(std::integral_constant<int, I>{}), I), __builtin_amdgcn_sched_barrier(0)), ...);
+    };
+    first_copies(std::make_integer_sequence<int, AHEAD ? NS : NS - 1>{});
     wait_vm<(AHEAD ? NS - 1 : NS - 2) * NI>();
     wait_lds();
     barrier();
@@ -643,12 +642,17 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         turn(s + 2, std::integral_constant<int, U + 2>{});
         turn(s + 3, std::integral_constant<int, U + 3>{});
     };
-    for (int s = 0; s < KS; s += NS) {
-        four(s, I0);
-        if constexpr (NS == 8) {
-            if (s + 4 >= KS) break;
+    if constexpr (NS == 4) {
+        for (int s = 0; s < KS; s += 4) four(s, I0);
+    } else {
+        // (with a way out in the middle of the loop the compiler no longer
+        // tells the stages apart, and waits for copies under way)
+        int s = 0;
+        for (; s + 4 < KS; s += 8) {
+            four(s, I0);
             four(s + 4, std::integral_constant<int, 4>{});
         }
+        if (s < KS) four(s, I0);
     }
     wait_vm<0>();
     wait_lds();
