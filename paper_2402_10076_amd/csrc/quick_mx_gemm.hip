@@ -363,67 +363,40 @@ __device__ __forceinline__ void dma16(rsrc_t r, void* dst, uint32_t voff, uint32
 // are read from LDS half a step (64 channels) before they are multiplied.
 // ONCE: the weights come past the caches.
 // TAIL: K is not a multiple of 128.
+struct Ring {
+    uint8_t *st0, *st1, *st2, *st3, *st4, *st5, *st6, *st7;
+};
+
 template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL, bool ONCE>
-__global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel(MxArgs a, int row_tiles)
+__device__ __forceinline__ void tiled_product(const MxArgs& a, Tile t, int nt, Ring ring)
 {
     constexpr int W = WM * WN, MB = BM / WM / 32, NB = BN / WN / 32;
     constexpr int XC = BM / 16, IM = (XC + W - 1) / W, IN = BN / 16 / W, NI = IM + IN;    // copies a wave and step
-    constexpr int STAGE = (BM + BN) * 64, XS = BM < 64 ? 64 : BM, SC = (XS + BN) * 16;
+    constexpr int STAGE = (BM + BN) * 64, XS = BM < 64 ? 64 : BM;
     static_assert(IN * W * 16 == BN && (NS == 4 || NS == 8), "weight copies are shared out evenly");
     // Operands go to registers a whole step before they are multiplied, but in
     // the largest tile, whose accumulators leave room for half a step.
     constexpr bool AHEAD = BM * BN < 65536;
-    constexpr int S8 = NS == 8 ? STAGE : 16;
-    // No more than eight objects, the number that the compiler tells apart in
-    // its waits: the scales lie behind the stages that are filled and read at
-    // the same turns
-    __shared__ __attribute__((aligned(16))) uint8_t st0[STAGE + SC], st1[STAGE], st2[STAGE], st3[STAGE],
-        st4[NS == 8 ? STAGE + SC : 16], st5[S8], st6[S8], st7[S8];
-    uint8_t* const sc0 = st0 + STAGE;
-    uint8_t* const sc1 = st4 + (NS == 8 ? STAGE : 0);
+    uint8_t* const sc0 = ring.st0 + STAGE;
+    uint8_t* const sc1 = ring.st4 + (NS == 8 ? STAGE : 0);
     auto scale_buffer = [&](auto which) __attribute__((always_inline)) -> uint8_t* {
         if constexpr (decltype(which)::value % (NS / 4) == 0) return sc0;
         else return sc1;
     };
     auto stage = [&](auto which) __attribute__((always_inline)) -> uint8_t* {
         constexpr int S = decltype(which)::value % NS;
-        if constexpr (S == 0) return st0;
-        else if constexpr (S == 1) return st1;
-        else if constexpr (S == 2) return st2;
-        else if constexpr (S == 3) return st3;
-        else if constexpr (S == 4) return st4;
-        else if constexpr (S == 5) return st5;
-        else if constexpr (S == 6) return st6;
-        else return st7;
+        if constexpr (S == 0) return ring.st0;
+        else if constexpr (S == 1) return ring.st1;
+        else if constexpr (S == 2) return ring.st2;
+        else if constexpr (S == 3) return ring.st3;
+        else if constexpr (S == 4) return ring.st4;
+        else if constexpr (S == 5) return ring.st5;
+        else if constexpr (S == 6) return ring.st6;
+        else return ring.st7;
     };
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wm = wave % WM, wn = wave / WM, col = lane & 31, half = lane >> 5;
 
-    // Workgroups go to the eight dies in turn: each die gets a run of tiles.
-    // A run goes over bands of eight row tiles, in a band over the column
-    // tiles, row tiles first: what is under way on a die at a time is near
-    // square, and shares its operands in the die's L2.
-    const int col_tiles = (a.N + BN - 1) / BN;
-    auto place = [&](int rows, int* mt, int* nt) {
-        const int per = (rows * col_tiles + 7) / 8, idx = blockIdx.x % 8 * per + blockIdx.x / 8;
-        if ((int)blockIdx.x / 8 >= per || idx >= rows * col_tiles) return false;
-        const int band = idx / (8 * col_tiles), in = idx - band * 8 * col_tiles, high = min(8, rows - 8 * band);
-        *nt = in / high;
-        *mt = band * 8 + in % high;
-        return true;
-    };
-    int mt, nt;
-    Tile t;
-    if constexpr (GRP) {
-        const GroupedTiles<BM> tiles(a);
-        if (!place(tiles.all, &mt, &nt)) return;
-        t = tiles.find(mt);
-    } else {
-        if (!place(row_tiles, &mt, &nt)) return;
-        t.m0 = mt * BM;
-        t.m1 = min(t.m0 + BM, a.M);
-        t.e = 0;
-    }
     const int KS = (a.K + 127) / 128, KQ = (KS + 3) / 4, KB = a.K / 32, NTT = (a.N + 15) / 16;
     const int64_t first = (int64_t)t.e * NTT + nt * (BN / 16);
     const int tiles = min(BN / 16, NTT - nt * (BN / 16));
@@ -513,6 +486,10 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     const int wr = BM * 64 + (wn * NB * 2 + (col >> 4)) * 1024 + half * 256 + (col & 15) * 16;
     const int xsr = (wm * MB * 32 + col) * 16;
     const int wsr = XS * 16 + (wn * NB * 2 + (col >> 4)) * 256 + (half * 16 + (col & 15)) * 4;
+    // the second word's address is kept apart: of two reads made one the
+    // compiler no longer knows the object, and waits for all copies under way
+    int wsr2 = wsr + 128;
+    asm volatile("" : "+v"(wsr2));
     u4_t x[AHEAD ? 4 : 2][MB], w[AHEAD ? 4 : 2][NB], xs[MB];
     uint32_t ws[NB][2];
     // half step h of a step: AHEAD keeps two steps, the odd ones in 2 and 3
@@ -535,9 +512,10 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
             for (int c = 0; c < 4; c++) to[i][c] = q * 4 + c < KS ? v[c] >> (8 * half) : 0;
         }
 #pragma unroll
-        for (int j = 0; j < NB; j++)
-#pragma unroll
-            for (int h = 0; h < 2; h++) tw[j][h] = *(const uint32_t*)(sc + wsr + j * 512 + h * 128);
+        for (int j = 0; j < NB; j++) {
+            tw[j][0] = *(const uint32_t*)(sc + wsr + j * 512);
+            tw[j][1] = *(const uint32_t*)(sc + wsr2 + j * 512);
+        }
     };
     auto multiply = [&](auto step, auto which) __attribute__((always_inline)) {
         constexpr int S = decltype(step)::value, h = decltype(which)::value, p = AHEAD ? S % 2 * 2 + h : h;
@@ -566,8 +544,8 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     wait_lds();
     barrier();
     read_scales(sc0, 0, xs, ws);
-    read(st0, I0, I0);
-    if constexpr (AHEAD) read(st0, I0, I1);
+    read(ring.st0, I0, I0);
+    if constexpr (AHEAD) read(ring.st0, I0, I1);
     // Order of a half step: one matrix instruction, then some of the LDS reads
     // and copies that are issued under it.
     auto interleave = [&](auto reads, auto copies) __attribute__((always_inline)) {
@@ -661,7 +639,7 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     // Rows of y of a wave's blocks go through LDS (a region of its own), from
     // where a lane takes 16 consecutive bytes.  Lane: row col of a block;
     // accumulator 4 b + c is column 8 b + 4 half + c.
-    uint8_t* mine = wave < (W + 1) / 2 ? st0 + wave * (NB * 2048) : st1 + (wave - (W + 1) / 2) * (NB * 2048);
+    uint8_t* mine = wave < (W + 1) / 2 ? ring.st0 + wave * (NB * 2048) : ring.st1 + (wave - (W + 1) / 2) * (NB * 2048);
     static_assert((W + 1) / 2 * NB * 2048 <= STAGE, "the waves' regions fit two stages");
     const uint16_t* bias = a.bias ? a.bias + (int64_t)t.e * a.N : nullptr;
     const int n0 = nt * BN + wn * NB * 32;
@@ -727,6 +705,54 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         if (a.bf16) finish(BF16, std::false_type{});
         else finish(F16, std::false_type{});
     }
+}
+
+template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL, bool ONCE>
+__global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel(MxArgs a, int row_tiles)
+{
+    constexpr int STAGE = (BM + BN) * 64, SC = ((BM < 64 ? 64 : BM) + BN) * 16, S8 = NS == 8 ? STAGE : 16;
+    // No more than eight objects, the number that the compiler tells apart in
+    // its waits: the scales lie behind the stages that are filled and read at
+    // the same turns
+    __shared__ __attribute__((aligned(16))) uint8_t st0[STAGE + SC], st1[STAGE], st2[STAGE], st3[STAGE],
+        st4[NS == 8 ? STAGE + SC : 16], st5[S8], st6[S8], st7[S8];
+    const Ring ring = {st0, st1, st2, st3, st4, st5, st6, st7};
+
+    // Workgroups go to the eight dies in turn: each die gets a run of tiles.
+    // A run goes over bands of eight row tiles, in a band over the column
+    // tiles, row tiles first: what is under way on a die at a time is near
+    // square, and shares its operands in the die's L2.
+    const int col_tiles = (a.N + BN - 1) / BN;
+    auto place = [&](int rows, int* mt, int* nt) {
+        const int per = (rows * col_tiles + 7) / 8, idx = blockIdx.x % 8 * per + blockIdx.x / 8;
+        if ((int)blockIdx.x / 8 >= per || idx >= rows * col_tiles) return false;
+        const int band = idx / (8 * col_tiles), in = idx - band * 8 * col_tiles, high = min(8, rows - 8 * band);
+        *nt = in / high;
+        *mt = band * 8 + in % high;
+        return true;
+    };
+    int mt, nt;
+    Tile t;
+    if constexpr (GRP) {
+        const GroupedTiles<BM> tiles(a);
+        if (!place(tiles.all, &mt, &nt)) return;
+        t = tiles.find(mt);
+    } else {
+        if (!place(row_tiles, &mt, &nt)) return;
+        t.m0 = mt * BM;
+        t.m1 = min(t.m0 + BM, a.M);
+        t.e = 0;
+    }
+    // A tile that is half empty or more, as an expert's last one often is, is
+    // multiplied as a lower one
+    if constexpr (BM >= 128) {
+        const int rows = uniform(t.m1 - t.m0);
+        if constexpr (BM >= 256) {
+            if (rows <= BM / 4) return tiled_product<BM / 4, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring);
+        }
+        if (rows <= BM / 2) return tiled_product<BM / 2, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring);
+    }
+    tiled_product<BM, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
