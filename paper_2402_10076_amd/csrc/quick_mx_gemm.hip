@@ -165,7 +165,9 @@ __device__ __forceinline__ void barrier()
 // column tiles.  A workgroup takes `groups` runs of NT column tiles one after
 // the other.  Operands go from memory straight into registers, D steps ahead,
 // also across the end of a run; at the end of one the waves' sums are added up
-// through LDS in the order of the waves, by waves that take turns.
+// through LDS in the order of the waves, by waves that take turns.  Bound by
+// the weights' bytes and the start of a launch (7B q, k, v, 26 MB, one row: 8.2
+// us with the quantisation; a copy kernel reads 26 MB in 6.8).
 // TAIL: K is not a multiple of 128; the blocks past its end are read as zero.
 // ONCE: the weights come past the caches.
 // XQ >= 0: activations x of that 16-bit type, at most kFusedRows rows; the
@@ -350,6 +352,12 @@ __device__ __forceinline__ void dma16(rsrc_t r, void* dst, uint32_t voff, uint32
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)dst, 16, voff, soff, 0, AUX);
 }
+
+// The stages of a tiled kernel in LDS.
+struct Ring {
+    uint8_t *st0, *st1, *st2, *st3, *st4, *st5, *st6, *st7;
+};
+
 // A BM x BN tile of y by WM x WN waves of MB x NB blocks of 32 x 32, on the
 // 32x32x64 instruction (twice the flops of the 16x16x128 one per operand byte
 // and issue slot).  Codes of both operands go from memory straight into LDS,
@@ -360,13 +368,14 @@ __device__ __forceinline__ void dma16(rsrc_t r, void* dst, uint32_t voff, uint32
 //    block (32 rows, one or two pieces) over all banks;
 //  * weights: one packed unit a copy, as it lies in memory.
 // The scales of four steps are copied together, into NS / 4 buffers.  Operands
-// are read from LDS half a step (64 channels) before they are multiplied.
+// are read from LDS a step, or half a one, before they are multiplied.
+// What bounds it: the largest tiles the power of the matrix instructions (2048
+// rows of 70B gate+up 464 us, 4.1 PFLOP/s; a loop of nothing but the
+// instruction on random operands reaches 6.4); the smaller ones the latency of
+// memory, a few stages of a tile's own columns being all that is under way
+// (333 rows of 13B down 25.9 us, 1.8 PFLOP/s).
 // ONCE: the weights come past the caches.
 // TAIL: K is not a multiple of 128.
-struct Ring {
-    uint8_t *st0, *st1, *st2, *st3, *st4, *st5, *st6, *st7;
-};
-
 template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL, bool ONCE>
 __device__ __forceinline__ void tiled_product(const MxArgs& a, Tile t, int nt, Ring ring)
 {
@@ -744,7 +753,8 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         t.e = 0;
     }
     // A tile that is half empty or more, as an expert's last one often is, is
-    // multiplied as a lower one
+    // multiplied as a lower one (4096 rows over 8 experts of 28672 x 4096:
+    // 358 us, 377 without)
     if constexpr (BM >= 128) {
         const int rows = uniform(t.m1 - t.m0);
         if constexpr (BM >= 256) {
@@ -842,23 +852,23 @@ int launch_tiled(const MxArgs& a, double expert_rows, hipStream_t hs)
 // stream form's `shared` counts column tiles plus activations (`rows` of a
 // column tile's cost for 16 rows).  Fitted to the times of all forms on 702
 // sizes (1 to 2048 rows, 512 to 57344 columns, 512 to 28672 channels, weights
-// from HBM), to 7 to 17 % each; the form chosen by it is 0.4 % slower than the
-// fastest of those measured on average, 14 % at most.
+// from HBM), to 8 to 25 % each; the form chosen by it is 0.2 % slower than the
+// fastest of those measured on average, 11 % at most.
 struct Form {
     int bm, bn;    // rows and columns of a tile
     float start, alone, shared, turn, stream, rows;
 };
 constexpr Form kForms[] = {
-    {16, 16, 2.80f, 0.0112f, 0.0262f, 0.521f, 5.14f, 1.60f},    // stream forms
-    {16, 32, 2.97f, 0.0415f, 0.0161f, 0.933f, 4.91f, 3.01f},
-    {16, 64, 2.68f, 0.0f, 0.0157f, 1.150f, 4.34f, 2.95f},
-    {32, 128, 1.28f, 0.2660f, 0.1610f, 1.67f, 5.13f, 0.0f},     // tiled forms
-    {64, 64, 2.42f, 0.0f, 0.1400f, 0.897f, 5.50f, 0.0f},        // eight stages
-    {64, 128, 0.53f, 0.0f, 0.1920f, 3.23f, 5.16f, 0.0f},        // eight stages
-    {64, 128, 2.19f, 0.2500f, 0.2030f, 1.05f, 5.14f, 0.0f},
-    {128, 128, 2.26f, 0.3150f, 0.2900f, 1.58f, 4.25f, 0.0f},
-    {128, 256, 0.0f, 0.1880f, 0.4330f, 4.58f, 4.09f, 0.0f},
-    {256, 256, 0.0f, 0.6530f, 0.5890f, 6.99f, 4.00f, 0.0f},
+    {16, 16, 3.05f, 0.0139f, 0.0265f, 0.453f, 5.26f, 1.52f},    // stream forms
+    {16, 32, 2.94f, 0.0428f, 0.0166f, 0.943f, 5.08f, 2.90f},
+    {16, 64, 2.59f, 0.0f, 0.0161f, 1.120f, 4.27f, 3.15f},
+    {32, 128, 1.12f, 0.1902f, 0.1602f, 1.55f, 5.55f, 0.0f},     // tiled forms
+    {64, 64, 2.04f, 0.0f, 0.1263f, 1.03f, 5.84f, 0.0f},         // eight stages
+    {64, 128, 0.11f, 0.0f, 0.1862f, 3.24f, 5.18f, 0.0f},        // eight stages
+    {64, 128, 1.68f, 0.2126f, 0.2049f, 1.08f, 5.49f, 0.0f},
+    {128, 128, 1.78f, 0.2444f, 0.2573f, 1.48f, 4.26f, 0.0f},
+    {128, 256, 0.0f, 0.2039f, 0.3873f, 4.31f, 4.16f, 0.0f},
+    {256, 256, 0.0f, 0.6207f, 0.5595f, 6.07f, 4.00f, 0.0f},
 };
 constexpr int kStreamForms = 3, kFormCount = 10;
 
