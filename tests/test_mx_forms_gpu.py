@@ -64,7 +64,8 @@ DENSE = [(1, 512, 1056), (3, 520, 2048), (1, 8192, 2048), (16, 5008, 1056), (1, 
          (16, 57344, 1056), (64, 2080, 4128), (1, 8200, 512), (30, 2050, 160), (7, 12320, 2048), (61, 12320, 4128),
          (33, 25601, 4096), (64, 25600, 4128), (40, 25600, 512), (100, 25604, 160), (150, 12320, 512),
          (333, 5120, 2080), (150, 25600, 512), (600, 13000, 1056), (260, 25600, 512), (2310, 8200, 1024),
-         (2100, 4112, 1056), (5000, 96, 288)]
+         (2100, 4112, 1056), (5000, 96, 288), (64, 2080, 8192), (50, 2080, 13856), (500, 2080, 4096), (200, 5120, 4128),
+         (150, 12320, 160), (2, 57344, 160)]
 
 
 @pytest.mark.parametrize("M,N,K", DENSE)
