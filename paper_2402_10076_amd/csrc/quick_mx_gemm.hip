@@ -1,10 +1,10 @@
 // Products with weights in microscaled 4-bit floating point on the scaled
-// 16x16x128 matrix instruction of gfx950.
+// matrix instructions of gfx950, 16x16x128 (few rows) and 32x32x64.
 //
 // y[m][n] = sum over blocks b of 2^(xs[m][b] + ws[n][b] - 254) *
 //           sum over the 32 channels of b of x[m][k] * w[n][k]
 //
-// The instruction takes, per lane, 32 consecutive channels of one row (16
+// The former takes, per lane, 32 consecutive channels of one row (16
 // bytes of codes, four registers) and that block's scale byte, for both
 // operands: lane l holds row l % 16 and block l / 16 of the step's four.  So a
 // 16-byte load of a row of codes is an operand as it stands, and so is a
@@ -41,6 +41,7 @@ struct MxArgs {
     int32_t T, E;              // rows of x, experts (grouped form)
     int32_t gated, bf16;
     int32_t wide;              // y is on 16 bytes
+    int32_t lead;              // 1: each column tile has a workgroup more, that writes nothing
 };
 
 __device__ __forceinline__ f4_t mx_mfma(u4_t a, u4_t b, f4_t c, uint32_t sa, uint32_t sb)
@@ -377,7 +378,7 @@ struct Ring {
 // ONCE: the weights come past the caches.
 // TAIL: K is not a multiple of 128.
 template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL, bool ONCE>
-__device__ __forceinline__ void tiled_product(const MxArgs& a, Tile t, int nt, Ring ring)
+__device__ __forceinline__ void tiled_product(const MxArgs& a, Tile t, int nt, Ring ring, bool leads)
 {
     constexpr int W = WM * WN, MB = BM / WM / 32, NB = BN / WN / 32;
     constexpr int XC = BM / 16, IM = (XC + W - 1) / W, IN = BN / 16 / W, NI = IM + IN;    // copies a wave and step
@@ -645,6 +646,8 @@ __device__ __forceinline__ void tiled_product(const MxArgs& a, Tile t, int nt, R
     wait_lds();
     __syncthreads();
 
+    if (leads) return;
+
     // Rows of y of a wave's blocks go through LDS (a region of its own), from
     // where a lane takes 16 consecutive bytes.  Lane: row col of a block;
     // accumulator 4 b + c is column 8 b + 4 half + c.
@@ -740,6 +743,10 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         *mt = band * 8 + in % high;
         return true;
     };
+    // A leading workgroup goes through its column's steps as the others do, on
+    // the last row alone, a little ahead of them.
+    constexpr bool LEAD = !GRP && NS == 8;
+    bool leads = false;
     int mt, nt;
     Tile t;
     if constexpr (GRP) {
@@ -747,8 +754,12 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         if (!place(tiles.all, &mt, &nt)) return;
         t = tiles.find(mt);
     } else {
-        if (!place(row_tiles, &mt, &nt)) return;
-        t.m0 = mt * BM;
+        if (!place(row_tiles + (LEAD ? a.lead : 0), &mt, &nt)) return;
+        if constexpr (LEAD) {
+            mt -= a.lead;
+            leads = mt < 0;
+        }
+        t.m0 = leads ? a.M - 1 : mt * BM;
         t.m1 = min(t.m0 + BM, a.M);
         t.e = 0;
     }
@@ -758,11 +769,11 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     if constexpr (BM >= 128) {
         const int rows = uniform(t.m1 - t.m0);
         if constexpr (BM >= 256) {
-            if (rows <= BM / 4) return tiled_product<BM / 4, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring);
+            if (rows <= BM / 4) return tiled_product<BM / 4, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring, leads);
         }
-        if (rows <= BM / 2) return tiled_product<BM / 2, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring);
+        if (rows <= BM / 2) return tiled_product<BM / 2, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring, leads);
     }
-    tiled_product<BM, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring);
+    tiled_product<BM, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring, leads);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -824,11 +835,27 @@ int launch_stream(const MxArgs& a, double expert_rows, int xq, hipStream_t hs)
     return QUICK_OK;
 }
 
-template <int BM, int BN, int WM, int WN, int NS, bool GRP>
-int launch_tiled(const MxArgs& a, double expert_rows, hipStream_t hs)
+// Whether the column tiles of an eight-stage form get a leading workgroup.
+// Where the row tiles of a column run in step, and none is light, all of them
+// wait for the same weights at a time; behind one that is ahead they find them
+// in L2 (128 x 4096 x 11008 20.8 -> 14.0 us, 256 x 5120 x 13824 31.5 -> 23.3,
+// 64 x 8192 x 28672 50.5 -> 37.4, all from HBM).  There has to be room for it:
+// past 256 workgroups (64 x 12288 x 4096, from 192 to 384: 10.5 -> 11.8), or
+// where 128 columns wide tiles pass 128, half of the compute units (256 x 4096
+// x 11008, from 128 to 160: 20.2 -> 26.0), it costs more than it gives.
+int has_lead(const MxArgs& a, int64_t tiles, int64_t columns, int bm, int bn)
 {
-    const int64_t rows = GRP ? a.M / BM + std::min(a.E, a.M) : ceil_div(a.M, BM);
-    const int64_t grid = ceil_div(rows * ceil_div(a.N, BN), 8) * 8;
+    const int light = a.M % bm;
+    const bool crosses = bn > 64 && tiles <= 128 && tiles + columns > 128;
+    return (light == 0 || light > bm / 4) && tiles + columns <= 256 && !crosses;
+}
+
+template <int BM, int BN, int WM, int WN, int NS, bool GRP>
+int launch_tiled(MxArgs a, double expert_rows, hipStream_t hs)
+{
+    const int64_t rows = GRP ? a.M / BM + std::min(a.E, a.M) : ceil_div(a.M, BM), columns = ceil_div(a.N, BN);
+    if (!GRP && NS == 8) a.lead = has_lead(a, rows * columns, columns, BM, BN);
+    const int64_t grid = ceil_div((rows + a.lead) * columns, 8) * 8;
     if (grid > (1 << 22)) return QUICK_ERR_SHAPE;
     const dim3 g((uint32_t)grid), block(64 * WM * WN);
     with_bool(a.K % 128 != 0, [&](auto tail) {
@@ -968,6 +995,7 @@ MxArgs make_args(const void* codes, const void* scales, const void* packed, cons
     a.gated = activation == QUICK_ACT_SILU_GATE;
     a.bf16 = dtype == QUICK_BF16;
     a.wide = aligned(y, 16);
+    a.lead = 0;
     return a;
 }
 
