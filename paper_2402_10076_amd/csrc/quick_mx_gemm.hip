@@ -745,7 +745,6 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     };
     // A leading workgroup goes through its column's steps as the others do, on
     // the last row alone, a little ahead of them.
-    constexpr bool LEAD = !GRP && NS == 8;
     bool leads = false;
     int mt, nt;
     Tile t;
@@ -754,11 +753,9 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
         if (!place(tiles.all, &mt, &nt)) return;
         t = tiles.find(mt);
     } else {
-        if (!place(row_tiles + (LEAD ? a.lead : 0), &mt, &nt)) return;
-        if constexpr (LEAD) {
-            mt -= a.lead;
-            leads = mt < 0;
-        }
+        if (!place(row_tiles + a.lead, &mt, &nt)) return;
+        mt -= a.lead;
+        leads = mt < 0;
         t.m0 = leads ? a.M - 1 : mt * BM;
         t.m1 = min(t.m0 + BM, a.M);
         t.e = 0;
@@ -835,26 +832,27 @@ int launch_stream(const MxArgs& a, double expert_rows, int xq, hipStream_t hs)
     return QUICK_OK;
 }
 
-// Whether the column tiles of an eight-stage form get a leading workgroup.
-// Where the row tiles of a column run in step, and none is light, all of them
-// wait for the same weights at a time; behind one that is ahead they find them
-// in L2 (128 x 4096 x 11008 20.8 -> 14.0 us, 256 x 5120 x 13824 31.5 -> 23.3,
-// 64 x 8192 x 28672 50.5 -> 37.4, all from HBM).  There has to be room for it:
-// past 256 workgroups (64 x 12288 x 4096, from 192 to 384: 10.5 -> 11.8), or
-// where 128 columns wide tiles pass 128, half of the compute units (256 x 4096
-// x 11008, from 128 to 160: 20.2 -> 26.0), it costs more than it gives.
+// Whether every column tile gets a leading workgroup.  Where the row tiles of a
+// column run in step, and none is light, all of them wait for the same weights
+// at a time; behind one that is ahead they find them in L2 (128 x 4096 x 11008
+// 20.8 -> 14.0 us, 64 x 8192 x 28672 50.5 -> 37.4, 512 x 5120 x 13824 43.7 ->
+// 31.9, 1536 x 8192 x 28672 193 -> 180, weights from HBM; with 1024 channels no
+// difference).  There has to be room for it: past one workgroup a compute unit
+// (64 x 12288 x 4096, from 192 to 384: 10.5 -> 11.8; 1024 x 8192 x 8192, from
+// 256 to 288: 42.7 -> 61.7), or where wide tiles pass half of the units (256 x
+// 4096 x 11008, from 128 to 160: 20.2 -> 26.0), it costs more than it gives.
 int has_lead(const MxArgs& a, int64_t tiles, int64_t columns, int bm, int bn)
 {
     const int light = a.M % bm;
     const bool crosses = bn > 64 && tiles <= 128 && tiles + columns > 128;
-    return (light == 0 || light > bm / 4) && tiles + columns <= 256 && !crosses;
+    return a.K >= 2048 && (light == 0 || light > bm / 4) && tiles + columns <= 256 && !crosses;
 }
 
 template <int BM, int BN, int WM, int WN, int NS, bool GRP>
 int launch_tiled(MxArgs a, double expert_rows, hipStream_t hs)
 {
     const int64_t rows = GRP ? a.M / BM + std::min(a.E, a.M) : ceil_div(a.M, BM), columns = ceil_div(a.N, BN);
-    if (!GRP && NS == 8) a.lead = has_lead(a, rows * columns, columns, BM, BN);
+    if (!GRP) a.lead = has_lead(a, rows * columns, columns, BM, BN);
     const int64_t grid = ceil_div((rows + a.lead) * columns, 8) * 8;
     if (grid > (1 << 22)) return QUICK_ERR_SHAPE;
     const dim3 g((uint32_t)grid), block(64 * WM * WN);

@@ -65,7 +65,11 @@ DENSE = [(1, 512, 1056), (3, 520, 2048), (1, 8192, 2048), (16, 5008, 1056), (1, 
          (33, 25601, 4096), (64, 25600, 4128), (40, 25600, 512), (100, 25604, 160), (150, 12320, 512),
          (333, 5120, 2080), (150, 25600, 512), (600, 13000, 1056), (260, 25600, 512), (2310, 8200, 1024),
          (2100, 4112, 1056), (5000, 96, 288), (64, 2080, 8192), (50, 2080, 13856), (500, 2080, 4096), (200, 5120, 4128),
-         (150, 12320, 160), (2, 57344, 160)]
+         (150, 12320, 160), (2, 57344, 160),
+         # with a leading workgroup of each column
+         (64, 1040, 2048), (512, 1056, 2080), (256, 4112, 4096), (512, 2080, 4128), (100, 10240, 2080), (512, 2080, 2048),
+         (512, 4112, 2048), (1024, 2080, 2080), (448, 10240, 2080), (1024, 4112, 2048), (1536, 6144, 2048),
+         (2048, 4112, 2048)]
 
 
 @pytest.mark.parametrize("M,N,K", DENSE)
