@@ -374,7 +374,7 @@ struct Ring {
 // rows of 70B gate+up 464 us, 4.1 PFLOP/s; a loop of nothing but the
 // instruction on random operands reaches 6.4); the smaller ones the latency of
 // memory, a few stages of a tile's own columns being all that is under way
-// (333 rows of 13B down 25.9 us, 1.8 PFLOP/s).
+// (333 rows of 13B down 25 us, 1.9 PFLOP/s).
 // ONCE: the weights come past the caches.
 // TAIL: K is not a multiple of 128.
 template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL, bool ONCE>
@@ -877,8 +877,9 @@ int launch_tiled(MxArgs a, double expert_rows, hipStream_t hs)
 // stream form's `shared` counts column tiles plus activations (`rows` of a
 // column tile's cost for 16 rows).  Fitted to the times of all forms on 702
 // sizes (1 to 2048 rows, 512 to 57344 columns, 512 to 28672 channels, weights
-// from HBM), to 8 to 25 % each; the form chosen by it is 0.2 % slower than the
-// fastest of those measured on average, 11 % at most.
+// from HBM), to 8 to 25 % each, without leading workgroups; with them the form
+// chosen by it is 0.5 % slower than the fastest of those measured on average,
+// 26 % at most (fitting anew gives 0.4).
 struct Form {
     int bm, bn;    // rows and columns of a tile
     float start, alone, shared, turn, stream, rows;
