@@ -23,8 +23,10 @@ __device__ __forceinline__ To bits_as(const From& v)
 }
 
 // Raw buffers: a wave-uniform descriptor (base, byte size), a per-lane byte
-// offset and a wave-uniform one.  A per-lane offset at or beyond the size
-// reads as zero and writes nothing; the uniform offset is not checked.
+// offset and a wave-uniform one.  What lies at or beyond the size by the
+// per-lane offset reads as zero, word by word; the uniform offset is added
+// behind that check (by the compiler's documentation), so a read that may
+// pass the end has all of its offset in the lane.
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 
 __device__ __forceinline__ rsrc_t make_rsrc(const void* p, uint32_t bytes)

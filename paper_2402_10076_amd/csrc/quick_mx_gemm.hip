@@ -18,6 +18,7 @@
 
 #include "quick_mx.h"
 #include "quick_mx_quant.h"
+#include "quick_mx_scales.h"
 
 namespace {
 
@@ -441,24 +442,22 @@ __device__ __forceinline__ void tiled_product(const MxArgs& a, Tile t, int nt, R
     // scales of four steps: a copy of 64 rows' 16 bytes each, and of four
     // weight tiles'; the last waves may repeat a copy
     constexpr int CM = XS / 64, CN = BN / 64, CI = (CM + CN + W - 1) / W;
-    uint32_t so[CI], sbytes[CI], sstep[CI];
+    uint32_t so[CI], sbytes[CI];
     const uint8_t* sbase[CI];
 #pragma unroll
     for (int i = 0; i < CI; i++) {
         const int c = min(i * W + wave, CM + CN - 1);
         const bool rows = c < CM;
-        so[i] = rows ? source(c * 64 + lane) * (uint32_t)KB
-                     : (uint32_t)((c - CM) * 4 + (lane >> 4)) * KQ * 256 + (lane & 15) * 16;
+        so[i] = rows ? row_scales(source(c * 64 + lane), KB) : tile_scales((c - CM) * 4 + (lane >> 4), KQ, lane);
         sbase[i] = uniform(rows ? a.scales : ps);
         sbytes[i] = uniform(rows ? xsbytes : wsbytes);
-        sstep[i] = uniform(rows ? 16u : 256u);
     }
     auto copy_scales = [&](uint8_t* sc, int q) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < CI; i++) {
             const int c = min(i * W + wave, CM + CN - 1);
-            if (!TAIL || c >= CM)
-                dma16<0>(make_rsrc(sbase[i], q < KQ ? sbytes[i] : 0), sc + c * 1024, so[i], q * sstep[i]);
+            const BufferPlace p = scale_copy(so[i], c < CM, q);
+            if (!TAIL || c >= CM) dma16<0>(make_rsrc(sbase[i], q < KQ ? sbytes[i] : 0), sc + c * 1024, p.lane, p.uniform);
         }
     };
     // TAIL: a row's scales start anywhere, and past its end is the next row's:
