@@ -20,6 +20,10 @@ Entry points mirror include/quick.h:
 * ``mxfp4_*``: microscaled 4-bit floating point (include/quick_mx.h, mx.py)
 * ``moe_route`` / ``moe_combine``: a mixture-of-experts layer's router and
   the sum over a token's experts (include/quick_moe.h, moe.py)
+
+``stream``, where an entry point has it, is a torch.cuda.Stream to run on in
+place of the current one: inputs, and outputs and workspaces that are given,
+have to be ready on it; what the call allocates itself is of its memory.
 """
 from __future__ import annotations
 
@@ -328,11 +332,29 @@ def _check_weights(what: str, x, packed, scales, zeros, K: int, N: int, group: i
     _dev(what, "zeros", zeros, x, nbytes=zb * experts)
 
 
-def _out(what: str, y, x, rows: int, cols: int):
+def _taken(stream, ref, make, kept=True):
+    """make()'s tensors, for a call on ``stream`` (None: the current one).
+
+    They are of that stream's memory: a block of the current stream's may
+    still be in use by work that waits there, and the call is not ordered
+    behind it.  Those that the caller keeps are recorded on the current
+    stream, where they may be read once it is ordered behind the call."""
+    if stream is None or not ref.is_cuda:
+        return make()
+    with torch.cuda.stream(stream):
+        made = make()
+    if kept:
+        now = torch.cuda.current_stream(ref.device)
+        for t in made:
+            t.record_stream(now)
+    return made
+
+
+def _out(what: str, y, x, rows: int, cols: int, stream=None):
     if y is None:
-        if type(x) is torch.Tensor:
+        if stream is None and type(x) is torch.Tensor:
             return x.new_empty((rows, cols))
-        return torch.empty((rows, cols), dtype=torch.float16, device=x.device)
+        return _taken(stream, x, lambda: (torch.empty((rows, cols), dtype=torch.float16, device=x.device),))[0]
     _dev(what, "y", y, x, dtype=torch.float16, shape=(rows, cols))
     return y
 
@@ -368,7 +390,7 @@ def w4a16_gemm(x: torch.Tensor, packed: torch.Tensor, scales: torch.Tensor, zero
     _check_x(what, x)
     M, K = x.shape
     _check_weights(what, x, packed, scales, zeros, K, N, group)
-    y = _out(what, y, x, M, N)
+    y = _out(what, y, x, M, N, stream)
     wsb = _ws(what, workspace, x)
     hs = _stream(stream, x)
     if cfg is None and workspace is None:
@@ -409,7 +431,7 @@ def tune(x: torch.Tensor, packed: torch.Tensor, scales: torch.Tensor, zeros: tor
     _check_x(what, x)
     M, K = x.shape
     _check_weights(what, x, packed, scales, zeros, K, N, group)
-    y = _out(what, y, x, M, N)
+    y = _out(what, y, x, M, N, stream)
     hs = _stream(stream, x)
     c = QuickConfig()
     _check(lib().quick_tune(_dptr(x), _dptr(packed), _dptr(scales), _dptr(zeros), _dptr(y), M, N, K, group,
@@ -490,7 +512,7 @@ def grouped_gemm(x: torch.Tensor, offsets: torch.Tensor, packed: torch.Tensor, s
     zeros: the experts' buffers back to back (``pack_experts`` + ``to_device``)."""
     what = "grouped_gemm"
     T, K, E, R = _grouped_args(what, x, offsets, rows, R, packed, scales, zeros, N, group)
-    y = _out(what, y, x, R, N)
+    y = _out(what, y, x, R, N, stream)
     wsb = _ws(what, workspace, x)
     hs = _stream(stream, x)
     args = (_dptr(x), _dptr(rows), _dptr(offsets), _dptr(packed), _dptr(scales), _dptr(zeros), _dptr(y),
@@ -547,7 +569,7 @@ def gemm_fused(x: torch.Tensor, packed: torch.Tensor, scales: torch.Tensor, zero
     M, K = x.shape
     _check_weights(what, x, packed, scales, zeros, K, N, group)
     _check_bias(what, bias, x, N)
-    y = _out(what, y, x, M, N // 2 if activation == ACT_SILU_GATE else N)
+    y = _out(what, y, x, M, N // 2 if activation == ACT_SILU_GATE else N, stream)
     wsb = _ws(what, workspace, x)
     hs = _stream(stream, x)
     e = _epi(bias, activation)
@@ -568,7 +590,7 @@ def grouped_gemm_fused(x: torch.Tensor, offsets: torch.Tensor, packed: torch.Ten
     what = "grouped_gemm_fused"
     T, K, E, R = _grouped_args(what, x, offsets, rows, R, packed, scales, zeros, N, group)
     _check_bias(what, bias, x, E * N)
-    y = _out(what, y, x, R, N // 2 if activation == ACT_SILU_GATE else N)
+    y = _out(what, y, x, R, N // 2 if activation == ACT_SILU_GATE else N, stream)
     wsb = _ws(what, workspace, x)
     hs = _stream(stream, x)
     e = _epi(bias, activation)

@@ -18,7 +18,7 @@ from typing import NamedTuple
 import torch
 
 import paper_2402_10076_amd as _q
-from paper_2402_10076_amd.mx import _TYPES, _TYPES16, _fail, _gpu, _plain, _type
+from paper_2402_10076_amd.mx import _TYPES, _TYPES16, _fail, _gpu, _new, _plain, _type
 
 SCORE_SOFTMAX = 0
 SCORE_SIGMOID = 1
@@ -86,10 +86,12 @@ def moe_route(logits: torch.Tensor, topk: int, score: int = SCORE_SOFTMAX, bias:
     if bias is not None:
         _q._dev(what, "bias", bias, logits, dtype=torch.float32, shape=(E,))
     if out is None:
-        dev = logits.device
-        ids = torch.empty((T, topk), dtype=torch.int32, device=dev)
-        out = Routing(ids, torch.empty((T, topk), dtype=torch.float32, device=dev), ids.new_empty(E + 1),
-                      ids.new_empty(T * topk), ids.new_empty((T, topk)))
+        def make():
+            dev = logits.device
+            ids = torch.empty((T, topk), dtype=torch.int32, device=dev)
+            return Routing(ids, torch.empty((T, topk), dtype=torch.float32, device=dev), ids.new_empty(E + 1),
+                           ids.new_empty(T * topk), ids.new_empty((T, topk)))
+        out = _q._taken(stream, logits, make)
     else:
         for name, shape in (("ids", (T, topk)), ("weights", (T, topk)), ("offsets", (E + 1,)), ("rows", (T * topk,)),
                             ("slots", (T, topk))):
@@ -100,9 +102,8 @@ def moe_route(logits: torch.Tensor, topk: int, score: int = SCORE_SOFTMAX, bias:
     if workspace is None:
         wsb = L.quick_moe_route_workspace_bytes(T, E, topk)
         if wsb:
-            workspace = torch.empty(wsb, dtype=torch.uint8, device=logits.device)
-            if stream is not None:
-                workspace.record_stream(stream)
+            workspace = _q._taken(stream, logits, lambda: torch.empty(wsb, dtype=torch.uint8, device=logits.device),
+                                  kept=False)
     else:
         _q._dev(what, "workspace", workspace, logits)
         wsb = workspace.nbytes
@@ -136,7 +137,7 @@ def moe_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, res
     if residual is not None and not (_plain(residual, dev, y.dtype) and residual.shape == (T, D)):
         _q._dev(what, "residual", residual, y, dtype=y.dtype, shape=(T, D))
     if out is None:
-        out = y.new_empty((T, D))
+        out = _new(stream, y, (T, D), y.dtype)
     else:
         _q._dev(what, "out", out, y, dtype=y.dtype, shape=(T, D))
     _q._check(_q.lib().quick_moe_combine(y.data_ptr(), dtype, R, D, slots.data_ptr(), weights.data_ptr(), T, topk,

@@ -49,6 +49,12 @@ def _fail(status, text, *a):
     raise _q.QuickError(status, text % a)
 
 
+def _new(stream, ref, shape, dtype):
+    if stream is None:
+        return ref.new_empty(shape, dtype=dtype)
+    return _q._taken(stream, ref, lambda: (ref.new_empty(shape, dtype=dtype),))[0]
+
+
 def _plain(t, device, dtype):
     """Whether _dev has nothing to say against t, for the usual case (a small
     call is bound by the host; _dev takes three times as long)."""
@@ -107,11 +113,11 @@ def mxfp4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: t
     if ldx < K:
         _fail(_q.QUICK_ERR_SHAPE, "%s: rows of x overlap (stride %d, K=%d)", what, ldx, K)
     if codes is None:
-        codes = x.new_empty((rows, K // 2), dtype=torch.uint8)
+        codes = _new(stream, x, (rows, K // 2), torch.uint8)
     else:
         _q._dev(what, "codes", codes, x, dtype=torch.uint8, shape=(rows, K // 2))
     if scales is None:
-        scales = x.new_empty((rows, K // MX_BLOCK), dtype=torch.uint8)
+        scales = _new(stream, x, (rows, K // MX_BLOCK), torch.uint8)
     else:
         _q._dev(what, "scales", scales, x, dtype=torch.uint8, shape=(rows, K // MX_BLOCK))
     _q._check(_q.lib().quick_mxfp4_quantize(x.data_ptr(), dtype, ldx, rows, K, codes.data_ptr(), scales.data_ptr(),
@@ -127,7 +133,7 @@ def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dty
     code = _type(what, "dtype", dtype, _TYPES)
     shape = (*codes.shape[:-1], K)
     if y is None:
-        y = codes.new_empty(shape, dtype=dtype)
+        y = _new(stream, codes, shape, dtype)
     else:
         _q._dev(what, "y", y, codes, dtype=dtype, shape=shape)
     _q._check(_q.lib().quick_mxfp4_dequantize(codes.data_ptr(), scales.data_ptr(), code,
@@ -164,8 +170,7 @@ def mxfp4_pack(codes: torch.Tensor, scales: torch.Tensor, gate_up: bool = False,
     E = codes.shape[0] if codes.dim() == 3 else 1
     pb, sb = _matrix_bytes(what, N, K)
     lead = (E,) if codes.dim() == 3 else ()
-    packed = torch.empty((*lead, pb), dtype=torch.uint8, device=codes.device)
-    pscales = torch.empty((*lead, sb), dtype=torch.uint8, device=codes.device)
+    packed, pscales = (_new(stream, codes, (*lead, n), torch.uint8) for n in (pb, sb))
     _q._check(_q.lib().quick_mxfp4_pack(codes.data_ptr(), scales.data_ptr(), E, N, K, int(bool(gate_up)),
                                         packed.data_ptr(), pscales.data_ptr(), _q._stream(stream, codes)),
               "quick_mxfp4_pack")
@@ -183,13 +188,13 @@ def _check_packed(what, ref, packed, pscales, N, K, E=1):
     _q._dev(what, "packed_scales", pscales, ref, nbytes=E * sb)
 
 
-def _out(what, y, ref, rows, N, activation, dtype):
+def _out(what, y, ref, rows, N, activation, dtype, stream):
     if activation == _q.ACT_SILU_GATE:
         if N % 32:
             _fail(_q.QUICK_ERR_SHAPE, "%s: gated columns come in tiles of 32 (N=%d)", what, N)
         N //= 2
     if y is None:
-        return ref.new_empty((rows, N), dtype=dtype)
+        return _new(stream, ref, (rows, N), dtype)
     _q._dev(what, "y", y, ref, dtype=dtype, shape=(rows, N))
     return y
 
@@ -218,7 +223,7 @@ def mxfp4_gemm(codes: torch.Tensor, scales: torch.Tensor, packed: torch.Tensor, 
     M = codes.shape[0]
     _check_packed(what, codes, packed, packed_scales, N, K)
     b = _bias(what, bias, codes, N, dtype)
-    y = _out(what, y, codes, M, N, activation, dtype)
+    y = _out(what, y, codes, M, N, activation, dtype, stream)
     _q._check(_q.lib().quick_mxfp4_gemm(codes.data_ptr(), scales.data_ptr(), packed.data_ptr(),
                                         packed_scales.data_ptr(), y.data_ptr(), code, M, N, K, b, int(activation),
                                         _q._stream(stream, codes)), "quick_mxfp4_gemm")
@@ -245,15 +250,13 @@ def mxfp4_linear(x: torch.Tensor, packed: torch.Tensor, packed_scales: torch.Ten
     _channels(what, K)
     _check_packed(what, x, packed, packed_scales, N, K)
     b = _bias(what, bias, x, N, x.dtype)
-    y = _out(what, y, x, M, N, activation, x.dtype)
+    y = _out(what, y, x, M, N, activation, x.dtype, stream)
     L = _q.lib()
     hs = _q._stream(stream, x)
     if workspace is None:
         wsb = L.quick_mxfp4_linear_workspace_bytes(M, N, K)
         if wsb:
-            workspace = x.new_empty(wsb, dtype=torch.uint8)
-            if stream is not None:
-                workspace.record_stream(stream)
+            workspace = _q._taken(stream, x, lambda: x.new_empty(wsb, dtype=torch.uint8), kept=False)
     else:
         _q._dev(what, "workspace", workspace, x)
         wsb = workspace.nbytes
@@ -293,7 +296,7 @@ def mxfp4_grouped_gemm(codes: torch.Tensor, scales: torch.Tensor, offsets: torch
     code = _type(what, "dtype", dtype, _TYPES16)
     _check_packed(what, codes, packed, packed_scales, N, K, E)
     b = _bias(what, bias, codes, E * N, dtype)
-    y = _out(what, y, codes, R, N, activation, dtype)
+    y = _out(what, y, codes, R, N, activation, dtype, stream)
     _q._check(_q.lib().quick_mxfp4_grouped_gemm(
         codes.data_ptr(), scales.data_ptr(), rows.data_ptr() if rows is not None else None, offsets.data_ptr(),
         packed.data_ptr(), packed_scales.data_ptr(), y.data_ptr(), code, T, R, E, N, K, b, int(activation),
