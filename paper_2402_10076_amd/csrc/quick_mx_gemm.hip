@@ -13,10 +13,10 @@
 // The weights are the A operand (result rows), so that a lane ends with four
 // consecutive columns of one row of y.
 #include <algorithm>
-#include <cmath>
 #include <type_traits>
 
 #include "quick_mx.h"
+#include "quick_mx_forms.h"
 #include "quick_mx_quant.h"
 #include "quick_mx_scales.h"
 
@@ -772,27 +772,6 @@ __global__ __launch_bounds__(64 * WM * WN, NS == 8 ? 1 : 2) void mx_tiled_kernel
     tiled_product<BM, BN, WM, WN, NS, GRP, TAIL, ONCE>(a, t, nt, ring, leads);
 }
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// Rows and values of activations that a product's own launch quantises: a
-// workgroup does it all, so it has to stay small beside its weights, and its
-// codes, with the sums of two column tiles, within 64 KiB of LDS.
-constexpr int kFusedRows = 4;
-constexpr int64_t kFusedValues = 57344;
-
-bool fused(int64_t M, int64_t K) { return M <= kFusedRows && M * K <= kFusedValues; }
-
-// Whether the weights come past the caches: where a tile of rows reads them
-// once, and they do not stay in the 256 MB cache from call to call anyway
-// (70B gate+up, 16 rows: 39.3 us, 42.5 through them; but 7B down, 23 MB and 16
-// rows, 10.5 against 8.0 where a call finds what the one before has left).
-constexpr int64_t kOnceBytes = (int64_t)192 << 20;
-
-bool weights_once(const MxArgs& a, double rows, int bm)
-{
-    return rows <= bm && (int64_t)std::min(a.E, a.M) * a.N * a.K / 2 >= kOnceBytes;
-}
-
 // f(std::true_type) or f(std::false_type).
 template <class F>
 void with_bool(bool b, F f)
@@ -804,151 +783,74 @@ void with_bool(bool b, F f)
 // About 1536 workgroups (six for each compute unit), fewer where there are not
 // so many column tiles; each takes as many runs as that leaves.
 template <int NT, bool GRP>
-int launch_stream(const MxArgs& a, double expert_rows, int xq, hipStream_t hs)
+int launch_stream(const MxArgs& a, const MxPlan& p, int xq, hipStream_t hs)
 {
     constexpr int WK = 8, D = NT == 4 ? 2 : 4;
-    const int64_t rows = GRP ? a.M / 16 + std::min(a.E, a.M) : ceil_div(a.M, 16);
+    const int64_t rows = p.row_tiles, runs = p.columns;
     if (rows > 65535) return QUICK_ERR_SHAPE;
-    const int64_t runs = ceil_div(ceil_div(a.N, 16), NT);
+    if (a.gated && NT % 2 != 0) return QUICK_ERR_UNSUPPORTED;
+    int st = QUICK_OK;
     const int groups = (int)ceil_div(runs, std::max<int64_t>(1, 1536 / rows));
     const dim3 grid((uint32_t)ceil_div(runs, groups), (uint32_t)rows), block(64 * WK);
-    with_bool(a.K % 128 != 0, [&](auto tail) {
-        with_bool(weights_once(a, expert_rows, 16), [&](auto once) {
+    with_bool(p.tail, [&](auto tail) {
+        with_bool(p.once, [&](auto once) {
             constexpr bool TAIL = decltype(tail)::value, ONCE = decltype(once)::value;
-            if constexpr (!GRP && NT <= 2) {
-                if (xq >= 0) {
-                    const size_t lds = (size_t)a.M * (a.K / 2 + a.K / 32);
-                    if (xq == QUICK_F16)
-                        mx_stream_kernel<NT, WK, D, false, TAIL, ONCE, QUICK_F16><<<grid, block, lds, hs>>>(a, groups);
-                    else
-                        mx_stream_kernel<NT, WK, D, false, TAIL, ONCE, QUICK_BF16><<<grid, block, lds, hs>>>(a, groups);
-                    return;
-                }
+            if (xq < 0) {
+                mx_stream_kernel<NT, WK, D, GRP, TAIL, ONCE, -1><<<grid, block, 0, hs>>>(a, groups);
+            } else if constexpr (!GRP && NT <= 2) {
+                const size_t lds = (size_t)a.M * (a.K / 2 + a.K / 32);
+                if (xq == QUICK_F16)
+                    mx_stream_kernel<NT, WK, D, false, TAIL, ONCE, QUICK_F16><<<grid, block, lds, hs>>>(a, groups);
+                else
+                    mx_stream_kernel<NT, WK, D, false, TAIL, ONCE, QUICK_BF16><<<grid, block, lds, hs>>>(a, groups);
+            } else {
+                st = QUICK_ERR_UNSUPPORTED;    // no codes to read
             }
-            mx_stream_kernel<NT, WK, D, GRP, TAIL, ONCE, -1><<<grid, block, 0, hs>>>(a, groups);
         });
     });
-    return QUICK_OK;
-}
-
-// Whether every column tile gets a leading workgroup.  Where the row tiles of a
-// column run in step, and none is light, all of them wait for the same weights
-// at a time; behind one that is ahead they find them in L2 (128 x 4096 x 11008
-// 20.8 -> 14.0 us, 64 x 8192 x 28672 50.5 -> 37.4, 512 x 5120 x 13824 43.7 ->
-// 31.9, 1536 x 8192 x 28672 193 -> 180, weights from HBM; with 1024 channels no
-// difference).  There has to be room for it: past one workgroup a compute unit
-// (64 x 12288 x 4096, from 192 to 384: 10.5 -> 11.8; 1024 x 8192 x 8192, from
-// 256 to 288: 42.7 -> 61.7), or where wide tiles pass half of the units (256 x
-// 4096 x 11008, from 128 to 160: 20.2 -> 26.0), it costs more than it gives.
-int has_lead(const MxArgs& a, int64_t tiles, int64_t columns, int bm, int bn)
-{
-    const int light = a.M % bm;
-    const bool crosses = bn > 64 && tiles <= 128 && tiles + columns > 128;
-    return a.K >= 2048 && (light == 0 || light > bm / 4) && tiles + columns <= 256 && !crosses;
+    return st;
 }
 
 template <int BM, int BN, int WM, int WN, int NS, bool GRP>
-int launch_tiled(MxArgs a, double expert_rows, hipStream_t hs)
+int launch_tiled(MxArgs a, const MxPlan& p, hipStream_t hs)
 {
-    const int64_t rows = GRP ? a.M / BM + std::min(a.E, a.M) : ceil_div(a.M, BM), columns = ceil_div(a.N, BN);
-    if (!GRP) a.lead = has_lead(a, rows * columns, columns, BM, BN);
-    const int64_t grid = ceil_div((rows + a.lead) * columns, 8) * 8;
+    a.lead = p.lead;
+    const int64_t grid = ceil_div((p.row_tiles + p.lead) * p.columns, 8) * 8;
     if (grid > (1 << 22)) return QUICK_ERR_SHAPE;
     const dim3 g((uint32_t)grid), block(64 * WM * WN);
-    with_bool(a.K % 128 != 0, [&](auto tail) {
-        with_bool(weights_once(a, expert_rows, BM), [&](auto once) {
+    int st = QUICK_OK;
+    with_bool(p.tail, [&](auto tail) {
+        with_bool(p.once, [&](auto once) {
             constexpr bool TAIL = decltype(tail)::value, ONCE = decltype(once)::value;
-            // no tail in the largest form: its accumulators leave no registers
-            // for it; and the tallest are for more rows than read weights once
-            if constexpr (!(TAIL && BM * BN >= 65536))
-                mx_tiled_kernel<BM, BN, WM, WN, NS, GRP, TAIL, ONCE && BM <= 64><<<g, block, 0, hs>>>(a, (int)rows);
+            // no tail in the largest form, weights past the caches in the lower
+            // ones alone (form_takes, plan_product)
+            if constexpr ((TAIL && BM * BN >= 65536) || (ONCE && BM > 64))
+                st = QUICK_ERR_UNSUPPORTED;
+            else
+                mx_tiled_kernel<BM, BN, WM, WN, NS, GRP, TAIL, ONCE><<<g, block, 0, hs>>>(a, (int)p.row_tiles);
         });
     });
-    return QUICK_OK;
-}
-
-// The forms of the product, and what a call in each takes (us):
-//   pipe   = start + max(KS * alone, tiles * (KS * shared + turn))
-//   memory = 2 + bytes of weights / stream,   time = (pipe^4 + memory^4)^(1/4)
-// with KS steps of 128 channels and the tiles of the busiest of 256 compute
-// units: `shared` is a step's share of the unit, `turn` what a tile takes
-// besides its steps, `alone` a step's latency where the unit has one tile.  A
-// stream form's `shared` counts column tiles plus activations (`rows` of a
-// column tile's cost for 16 rows).  Fitted to the times of all forms on 702
-// sizes (1 to 2048 rows, 512 to 57344 columns, 512 to 28672 channels, weights
-// from HBM), to 8 to 25 % each, without leading workgroups; with them the form
-// chosen by it is 0.5 % slower than the fastest of those measured on average,
-// 26 % at most (fitting anew gives 0.4).
-struct Form {
-    int bm, bn;    // rows and columns of a tile
-    float start, alone, shared, turn, stream, rows;
-};
-constexpr Form kForms[] = {
-    {16, 16, 3.05f, 0.0139f, 0.0265f, 0.453f, 5.26f, 1.52f},    // stream forms
-    {16, 32, 2.94f, 0.0428f, 0.0166f, 0.943f, 5.08f, 2.90f},
-    {16, 64, 2.59f, 0.0f, 0.0161f, 1.120f, 4.27f, 3.15f},
-    {32, 128, 1.12f, 0.1902f, 0.1602f, 1.55f, 5.55f, 0.0f},     // tiled forms
-    {64, 64, 2.04f, 0.0f, 0.1263f, 1.03f, 5.84f, 0.0f},         // eight stages
-    {64, 128, 0.11f, 0.0f, 0.1862f, 3.24f, 5.18f, 0.0f},        // eight stages
-    {64, 128, 1.68f, 0.2126f, 0.2049f, 1.08f, 5.49f, 0.0f},
-    {128, 128, 1.78f, 0.2444f, 0.2573f, 1.48f, 4.26f, 0.0f},
-    {128, 256, 0.0f, 0.2039f, 0.3873f, 4.31f, 4.16f, 0.0f},
-    {256, 256, 0.0f, 0.6207f, 0.5595f, 6.07f, 4.00f, 0.0f},
-};
-constexpr int kStreamForms = 3, kFormCount = 10;
-
-double form_cost(const Form& f, bool stream, double tiles, double rows, int64_t KS, double bytes)
-{
-    double shared = f.shared;
-    if (stream) shared *= f.bn / 16 + f.rows * std::min(rows, 16.0) / 16;
-    const double pipe = f.start + std::max(KS * (double)f.alone, std::ceil(tiles / 256) * (KS * shared + f.turn));
-    const double memory = 2.0 + bytes / (f.stream * 1e6);
-    return pipe * pipe * pipe * pipe + memory * memory * memory * memory;
-}
-
-// The form of a product of `rows` rows with each of `experts` matrices.
-int choose_form(double rows, int64_t experts, int64_t N, int64_t K, bool gated, bool fused_only)
-{
-    int best = -1;
-    double least = 0;
-    // K's tail is not built into the largest form, nor quantisation into any
-    // but the first two
-    const int count = fused_only ? 2 : K % 128 ? kFormCount - 1 : kFormCount;
-    for (int i = 0; i < count; i++) {
-        if (gated && kForms[i].bn < 32) continue;    // a gate tile and its up tile in one wave
-        // an expert's last tile is half empty on average
-        const double high = experts > 1 ? std::max(1.0, rows / kForms[i].bm + 0.5) : std::ceil(rows / kForms[i].bm);
-        const double tiles = high * experts * ceil_div(N, kForms[i].bn);
-        const double c = form_cost(kForms[i], i < kStreamForms, tiles, rows, ceil_div(K, 128),
-                                   (double)experts * N * K * 17 / 32);
-        if (best < 0 || c < least) {
-            best = i;
-            least = c;
-        }
-    }
-    return best;
+    return st;
 }
 
 // xq >= 0: the activations are 16-bit values of that type, and few.
 template <bool GRP>
 int launch_mx(const MxArgs& a, int xq, hipStream_t hs)
 {
-    const int64_t busy = GRP ? std::min(a.E, a.M) : 1;
-    const double rows = (double)a.M / busy;
-    const int form = choose_form(rows, busy, a.N, a.K, a.gated, xq >= 0);
+    const MxPlan p = plan_product({a.M, a.N, a.K, a.E, GRP, a.gated != 0, xq >= 0});
     (void)hipGetLastError();
-    int st = QUICK_OK;
-    switch (form) {
-    case 0: st = launch_stream<1, GRP>(a, rows, xq, hs); break;
-    case 1: st = launch_stream<2, GRP>(a, rows, xq, hs); break;
-    case 2: st = launch_stream<4, GRP>(a, rows, xq, hs); break;
-    case 3: st = launch_tiled<32, 128, 1, 4, 4, GRP>(a, rows, hs); break;
-    case 4: st = launch_tiled<64, 64, 2, 2, 8, GRP>(a, rows, hs); break;
-    case 5: st = launch_tiled<64, 128, 1, 4, 8, GRP>(a, rows, hs); break;
-    case 6: st = launch_tiled<64, 128, 1, 4, 4, GRP>(a, rows, hs); break;
-    case 7: st = launch_tiled<128, 128, 2, 2, 4, GRP>(a, rows, hs); break;
-    case 8: st = launch_tiled<128, 256, 2, 4, 4, GRP>(a, rows, hs); break;
-    default: st = launch_tiled<256, 256, 2, 4, 4, GRP>(a, rows, hs); break;
+    int st = QUICK_ERR_UNSUPPORTED;
+    switch (p.form) {
+    case 0: st = launch_stream<1, GRP>(a, p, xq, hs); break;
+    case 1: st = launch_stream<2, GRP>(a, p, xq, hs); break;
+    case 2: st = launch_stream<4, GRP>(a, p, xq, hs); break;
+    case 3: st = launch_tiled<32, 128, 1, 4, 4, GRP>(a, p, hs); break;
+    case 4: st = launch_tiled<64, 64, 2, 2, 8, GRP>(a, p, hs); break;
+    case 5: st = launch_tiled<64, 128, 1, 4, 8, GRP>(a, p, hs); break;
+    case 6: st = launch_tiled<64, 128, 1, 4, 4, GRP>(a, p, hs); break;
+    case 7: st = launch_tiled<128, 128, 2, 2, 4, GRP>(a, p, hs); break;
+    case 8: st = launch_tiled<128, 256, 2, 4, 4, GRP>(a, p, hs); break;
+    case 9: st = launch_tiled<256, 256, 2, 4, 4, GRP>(a, p, hs); break;
     }
     return st ? st : launched();
 }
@@ -1016,7 +918,7 @@ extern "C" int quick_mxfp4_gemm(const void* codes, const void* scales, const voi
 
 extern "C" size_t quick_mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K)
 {
-    if (M <= 0 || fused(M, K) || check_product(M, M, N, K, QUICK_F16, QUICK_ACT_NONE)) return 0;
+    if (M <= 0 || fused_quantisation(M, K) || check_product(M, M, N, K, QUICK_F16, QUICK_ACT_NONE)) return 0;
     return code_bytes(M, K) + (size_t)(M * (K / 32));
 }
 
