@@ -21,8 +21,11 @@
  * K must be a positive multiple of 32 (SHAPE otherwise), any number of rows
  * and columns is accepted within these limits (SHAPE beyond):
  * rows <= 2^24, K <= 2^22, N <= 2^24; for quantisation and its inverse rows *
- * (K / 8192 rounded up) < 2^24; for a product rows * K < 2^33 activations and
- * N * K < 2^33 weights of one matrix.
+ * (K / 8192 rounded up) < 2^24; for a product rows * K < 2^33 activations,
+ * N * K < 2^33 weights of one matrix, at most 2^22 rows of y, and at most 2^22
+ * tiles of the size that the call is given: a dense product keeps that with
+ * (M + 64) * (N + 128) <= 2^34, one over experts with (R / 32 + E) * (N + 128)
+ * <= 2^28.
  */
 #ifndef QUICK_MX_H
 #define QUICK_MX_H
@@ -99,7 +102,8 @@ int quick_mxfp4_gemm(const void* codes, const void* scales, const void* packed, 
                      int dtype, int64_t M, int64_t N, int64_t K, const void* bias, int activation, void* stream);
 
 /* The same with 16-bit activations x [M][K] of y's type, quantised as by
- * quick_mxfp4_quantize on the way (the results are those of the two calls):
+ * quick_mxfp4_quantize on the way (the results are those of the two calls, up
+ * to the order of the sums):
  * inside the product's launch for few rows, otherwise into the workspace.
  * x: 16-byte aligned, contiguous.  workspace: 16-byte aligned, of
  * quick_mxfp4_linear_workspace_bytes() (0 when none is needed: may be NULL);
@@ -115,7 +119,7 @@ size_t quick_mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
  * offsets, T, R and E as in quick_w4a16_grouped_gemm (rows NULL: row r reads
  * x[r]); values that break that contract are clamped, and rows that no expert
  * owns are left as they were.  packed and packed_scales: the experts' back to
- * back, as quick_mxfp4_pack writes them; bias [E][N].  T, R <= 2^22.
+ * back, as quick_mxfp4_pack writes them; bias [E][N].
  * R == 0 is a valid no-op.  Errors: INVALID_ARG, SHAPE, ALIGNMENT, HIP. */
 int quick_mxfp4_grouped_gemm(const void* codes, const void* scales, const int32_t* rows, const int32_t* offsets,
                              const void* packed, const void* packed_scales, void* y, int dtype, int64_t T, int64_t R,

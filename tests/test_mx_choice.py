@@ -4,6 +4,7 @@ import subprocess
 import numpy as np
 
 import mx_plan
+import paper_2402_10076_amd as Q
 
 # Every form in turn made the cheapest of all, and put at every place of the
 # table: the choice has to be a form that is built for the call.
@@ -68,3 +69,52 @@ def test_plans_are_within_what_the_kernels_are_built_for(tmp_path):
         assert not (p["tail"] and p["form"] == 9) and not (gated and p["form"] == 0) and not (x16 and p["form"] > 1)
         assert not (p["once"] and p["bm"] > 64) and not (p["lead"] and (grouped or p["form"] < 3))
         assert p["form"] > 2 or p["row_tiles"] <= 65535
+
+
+def _accepted(s, p):
+    """As the launches check a grid."""
+    if p["form"] < 3:
+        return p["row_tiles"] <= 65535
+    return -(-(p["row_tiles"] + p["lead"]) * p["columns"] // 8) * 8 <= 1 << 22
+
+
+def test_sizes_within_the_header_s_limits_are_accepted(tmp_path):
+    g = np.random.Generator(np.random.PCG64(2))
+    sizes, beyond = [], []
+    for u in g.random((60000, 6)):
+        grouped, gated = int(u[0] < 0.5), int(u[1] < 0.3)
+        M, N, K = int((1 << 22) ** u[2]), int((1 << 24) ** u[3]), int((1 << 17) ** u[4]) * 32
+        E = int(512 ** u[5]) if grouped else 1
+        N = -(-N // 32) * 32 if gated else N
+        if max(M, N) * K >= 1 << 33:
+            continue
+        within = (M // 32 + E) * (N + 128) <= 1 << 28 if grouped else (M + 64) * (N + 128) <= 1 << 34
+        (sizes if within else beyond).append((M, N, K, E, grouped, gated, 0))
+    # on the lines themselves
+    for m in range(23):
+        for k in (32, 512, 2048):
+            n = min((1 << 34) // ((1 << m) + 64) - 128, 1 << 24, ((1 << 33) - 1) // k)
+            if n > 0 and k << m < 1 << 33:
+                sizes.append((1 << m, n, k, 1, 0, 0, 0))
+            for e in (2, 64, 512):
+                n = min((1 << 28) // ((1 << m) // 32 + e) - 128, 1 << 24, ((1 << 33) - 1) // k)
+                if n > 0 and k << m < 1 << 33:
+                    sizes.append((1 << m, n, k, e, 1, 0, 0))
+    assert all(_accepted(s, p) for s, p in zip(sizes, mx_plan.plans(tmp_path, sizes)))
+    # ... and past them some are not
+    assert not all(_accepted(s, p) for s, p in zip(beyond, mx_plan.plans(tmp_path, beyond)))
+
+
+def test_limits_of_the_calls():
+    """The library's own answers at the limits of rows, before anything is launched."""
+    L, a = Q.lib(), 0x10000
+
+    def grouped(t, r, n=32, k=32, y=0):
+        return L.quick_mxfp4_grouped_gemm(a, a, a, a, a, a, y, 0, t, r, 2, n, k, None, 0, None)
+
+    def gemm(m, n=32, k=32):
+        return L.quick_mxfp4_gemm(a, a, a, a, 0, 0, m, n, k, None, 0, None)
+    # accepted: the next thing that is found wrong is the missing y
+    assert gemm(1 << 22) == grouped(1 << 24, 1 << 22) == gemm(1, 1 << 24) == Q.QUICK_ERR_INVALID_ARG
+    assert gemm((1 << 22) + 1) == grouped(1 << 24, (1 << 22) + 1) == Q.QUICK_ERR_SHAPE
+    assert grouped((1 << 24) + 1, 1) == gemm(1, (1 << 24) + 1) == Q.QUICK_ERR_SHAPE
