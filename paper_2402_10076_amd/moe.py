@@ -60,6 +60,12 @@ def _options(*fields):
     return QuickRoute(*fields)
 
 
+def _routing(dev, T, E, topk):
+    ids = torch.empty((T, topk), dtype=torch.int32, device=dev)
+    return Routing(ids, torch.empty((T, topk), dtype=torch.float32, device=dev), ids.new_empty(E + 1),
+                   ids.new_empty(T * topk), ids.new_empty((T, topk)))
+
+
 def moe_route_workspace_bytes(T: int, E: int, topk: int) -> int:
     return int(_q.lib().quick_moe_route_workspace_bytes(T, E, topk))
 
@@ -86,12 +92,10 @@ def moe_route(logits: torch.Tensor, topk: int, score: int = SCORE_SOFTMAX, bias:
     if bias is not None:
         _q._dev(what, "bias", bias, logits, dtype=torch.float32, shape=(E,))
     if out is None:
-        def make():
-            dev = logits.device
-            ids = torch.empty((T, topk), dtype=torch.int32, device=dev)
-            return Routing(ids, torch.empty((T, topk), dtype=torch.float32, device=dev), ids.new_empty(E + 1),
-                           ids.new_empty(T * topk), ids.new_empty((T, topk)))
-        out = _q._taken(stream, logits, make)
+        if stream is None:
+            out = _routing(logits.device, T, E, topk)
+        else:
+            out = _q._taken(stream, logits, lambda: _routing(logits.device, T, E, topk))
     else:
         for name, shape in (("ids", (T, topk)), ("weights", (T, topk)), ("offsets", (E + 1,)), ("rows", (T * topk,)),
                             ("slots", (T, topk))):
@@ -102,8 +106,10 @@ def moe_route(logits: torch.Tensor, topk: int, score: int = SCORE_SOFTMAX, bias:
     if workspace is None:
         wsb = L.quick_moe_route_workspace_bytes(T, E, topk)
         if wsb:
-            workspace = _q._taken(stream, logits, lambda: torch.empty(wsb, dtype=torch.uint8, device=logits.device),
-                                  kept=False)
+            if stream is None:
+                workspace = torch.empty(wsb, dtype=torch.uint8, device=logits.device)
+            else:
+                workspace = _q._taken(stream, logits, lambda: logits.new_empty(wsb, dtype=torch.uint8), kept=False)
     else:
         _q._dev(what, "workspace", workspace, logits)
         wsb = workspace.nbytes
@@ -137,7 +143,7 @@ def moe_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, res
     if residual is not None and not (_plain(residual, dev, y.dtype) and residual.shape == (T, D)):
         _q._dev(what, "residual", residual, y, dtype=y.dtype, shape=(T, D))
     if out is None:
-        out = _new(stream, y, (T, D), y.dtype)
+        out = y.new_empty((T, D)) if stream is None else _new(stream, y, (T, D), y.dtype)
     else:
         _q._dev(what, "out", out, y, dtype=y.dtype, shape=(T, D))
     _q._check(_q.lib().quick_moe_combine(y.data_ptr(), dtype, R, D, slots.data_ptr(), weights.data_ptr(), T, topk,

@@ -50,8 +50,8 @@ def _fail(status, text, *a):
 
 
 def _new(stream, ref, shape, dtype):
-    if stream is None:
-        return ref.new_empty(shape, dtype=dtype)
+    """An empty tensor for a call on a given stream (on the current one a small
+    call, bound by the host, asks for it without this detour)."""
     return _q._taken(stream, ref, lambda: (ref.new_empty(shape, dtype=dtype),))[0]
 
 
@@ -113,11 +113,13 @@ def mxfp4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: t
     if ldx < K:
         _fail(_q.QUICK_ERR_SHAPE, "%s: rows of x overlap (stride %d, K=%d)", what, ldx, K)
     if codes is None:
-        codes = _new(stream, x, (rows, K // 2), torch.uint8)
+        shape = (rows, K // 2)
+        codes = x.new_empty(shape, dtype=torch.uint8) if stream is None else _new(stream, x, shape, torch.uint8)
     else:
         _q._dev(what, "codes", codes, x, dtype=torch.uint8, shape=(rows, K // 2))
     if scales is None:
-        scales = _new(stream, x, (rows, K // MX_BLOCK), torch.uint8)
+        shape = (rows, K // MX_BLOCK)
+        scales = x.new_empty(shape, dtype=torch.uint8) if stream is None else _new(stream, x, shape, torch.uint8)
     else:
         _q._dev(what, "scales", scales, x, dtype=torch.uint8, shape=(rows, K // MX_BLOCK))
     _q._check(_q.lib().quick_mxfp4_quantize(x.data_ptr(), dtype, ldx, rows, K, codes.data_ptr(), scales.data_ptr(),
@@ -133,7 +135,7 @@ def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dty
     code = _type(what, "dtype", dtype, _TYPES)
     shape = (*codes.shape[:-1], K)
     if y is None:
-        y = _new(stream, codes, shape, dtype)
+        y = codes.new_empty(shape, dtype=dtype) if stream is None else _new(stream, codes, shape, dtype)
     else:
         _q._dev(what, "y", y, codes, dtype=dtype, shape=shape)
     _q._check(_q.lib().quick_mxfp4_dequantize(codes.data_ptr(), scales.data_ptr(), code,
@@ -194,7 +196,7 @@ def _out(what, y, ref, rows, N, activation, dtype, stream):
             _fail(_q.QUICK_ERR_SHAPE, "%s: gated columns come in tiles of 32 (N=%d)", what, N)
         N //= 2
     if y is None:
-        return _new(stream, ref, (rows, N), dtype)
+        return ref.new_empty((rows, N), dtype=dtype) if stream is None else _new(stream, ref, (rows, N), dtype)
     _q._dev(what, "y", y, ref, dtype=dtype, shape=(rows, N))
     return y
 
@@ -256,7 +258,10 @@ def mxfp4_linear(x: torch.Tensor, packed: torch.Tensor, packed_scales: torch.Ten
     if workspace is None:
         wsb = L.quick_mxfp4_linear_workspace_bytes(M, N, K)
         if wsb:
-            workspace = _q._taken(stream, x, lambda: x.new_empty(wsb, dtype=torch.uint8), kept=False)
+            if stream is None:
+                workspace = x.new_empty(wsb, dtype=torch.uint8)
+            else:
+                workspace = _q._taken(stream, x, lambda: x.new_empty(wsb, dtype=torch.uint8), kept=False)
     else:
         _q._dev(what, "workspace", workspace, x)
         wsb = workspace.nbytes
