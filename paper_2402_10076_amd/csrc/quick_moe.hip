@@ -192,8 +192,9 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, int* l
 // which is the lowest expert.  Returns to lane j its j-th expert and weight.
 // Every sum is taken over a lane's places, then across the lanes: one order.
 // A token is some 600 vector instructions of its wave (256 experts in groups,
-// 8 choices), and that is the bound: 8192 such tokens 14.4 us (with a maximum
-// over all places in each of the topk turns and the groups through LDS 17.3).
+// 8 choices), and that is the bound of many: 8192 such tokens 14.0 us (with a
+// maximum over all places in each of the topk turns and the groups through LDS
+// 17.3).
 template <int DT, int W, int V>
 __device__ __forceinline__ void choose(const RouteArgs& a, int t, int lane, int* lds, int* my_id, float* my_weight)
 {
@@ -365,8 +366,9 @@ __device__ __forceinline__ void place_entries(const RouteArgs& a, int64_t first,
 
 // Choices of a workgroup's tokens, 64 / W tokens a wave at a time.  With one
 // workgroup also the sorted order; otherwise its counts.
-// Latency bound: a token is a chain of topk maxima over lanes, so a workgroup
-// takes few tokens (16 waves of 64 / W) and the launch as many workgroups.
+// A few tokens are bound by latency, each being a chain of topk maxima over
+// lanes, so a workgroup takes few of them (16 waves of 64 / W) and the launch as
+// many workgroups; many tokens by the vector instructions (choose).
 template <int DT, int W, int V>
 __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a)
 {

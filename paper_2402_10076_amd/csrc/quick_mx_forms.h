@@ -26,9 +26,14 @@ inline bool fused_quantisation(int64_t M, int64_t K) { return M <= kFusedRows &&
 // stream form's `shared` counts column tiles plus activations (`rows` of a
 // column tile's cost for 16 rows).  Fitted to the times of all forms on 702
 // sizes (1 to 2048 rows, 512 to 57344 columns, 512 to 28672 channels, weights
-// from HBM), to 8 to 25 % each, without leading workgroups; with them the form
-// chosen by it is 0.5 % slower than the fastest of those measured on average,
-// 26 % at most (fitting anew gives 0.4).
+// from HBM) without leading workgroups: 8 to 24 % (rms) a form over all of
+// them.  Past 4e11 operations, where the clock falls, the three largest forms
+// take 1.3 to 1.4 times what it says (2048 x 57344 x 8192: 457 us, 293 by it),
+// all of them, so that the order holds: of 21 such sizes the form chosen is at
+// most 0.8 % slower than the fastest.  Over all sizes, with leading workgroups,
+// that is 0.5 % on average and 26 % at most (fitting anew gives 0.4).  Over
+// experts, whose rows are taken as equal, it was 0 to 11 % on nine sizes (8192
+// rows over 32 experts of 5760 x 2880: 179 us, 162 in 128 x 256).
 struct Form {
     int bm, bn;    // rows and columns of a tile
     float start, alone, shared, turn, stream, rows;

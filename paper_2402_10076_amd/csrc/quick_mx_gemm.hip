@@ -371,11 +371,13 @@ struct Ring {
 //  * weights: one packed unit a copy, as it lies in memory.
 // The scales of four steps are copied together, into NS / 4 buffers.  Operands
 // are read from LDS a step, or half a one, before they are multiplied.
-// What bounds it: the largest tiles the power of the matrix instructions (2048
-// rows of 70B gate+up 464 us, 4.1 PFLOP/s; a loop of nothing but the
-// instruction on random operands reaches 6.4); the smaller ones the latency of
-// memory, a few stages of a tile's own columns being all that is under way
-// (333 rows of 13B down 25 us, 1.9 PFLOP/s).
+// What bounds it: the largest tiles the clock, 1.7 GHz under their power, and at
+// that clock the waits: the matrix instructions are busy 59 % of the cycles, a
+// wave waits for a barrier or for a count 30 % of its time (2048 rows of 70B
+// gate+up 464 us, 4.1 PFLOP/s; a loop of nothing but the instruction on random
+// operands reaches 6.4, at 1.5 GHz); the smaller ones the latency of memory, a
+// few stages of a tile's own columns being all that is under way (333 rows of
+// 13B down 24 us, 2.0 PFLOP/s).
 // ONCE: the weights come past the caches.
 // TAIL: K is not a multiple of 128.
 template <int BM, int BN, int WM, int WN, int NS, bool GRP, bool TAIL, bool ONCE>
