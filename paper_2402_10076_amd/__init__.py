@@ -20,6 +20,10 @@ Entry points mirror include/quick.h:
 * ``mxfp4_*``: microscaled 4-bit floating point (include/quick_mx.h, mx.py)
 * ``moe_route`` / ``moe_combine``: a mixture-of-experts layer's router and
   the sum over a token's experts (include/quick_moe.h, moe.py)
+* ``rotary``, ``kv4_*``: rotary positions, a paged 4-bit cache and attention
+  over it (include/quick_attention.h, attention.py)
+* ``lora_group`` / ``lora_add``: low-rank adapters of many requests beside a
+  shared projection (include/quick_lora.h, lora.py)
 
 ``stream``, where an entry point has it, is a torch.cuda.Stream to run on in
 place of the current one: inputs, and outputs and workspaces that are given,
@@ -175,6 +179,8 @@ def lib():
             L.quick_interleave_gate_up.restype = I
             mx._declare(L)
             moe._declare(L)
+            attention._declare(L)
+            lora._declare(L)
             _lib = L
     return _lib
 
@@ -632,10 +638,13 @@ EXPORTED = (
 )
 
 # the modules call this one's helpers, so they come last
-from . import moe, mx  # noqa: E402
+from . import attention, lora, moe, mx  # noqa: E402
+from .attention import (KV4_DIMS, KV4_PAGE, kv4_attention, kv4_attention_workspace_bytes, kv4_cache,  # noqa: E402
+                        kv4_read, kv4_write, rotary, rotary_frequencies)
+from .lora import LORA_MAX_RANK, lora_add, lora_group, lora_workspace_bytes  # noqa: E402
 from .moe import (MAX_EXPERTS, MAX_GROUPS, MAX_TOPK, SCORE_SIGMOID, SCORE_SOFTMAX, Routing, moe_combine,  # noqa: E402
                   moe_route, moe_route_workspace_bytes)
 from .mx import (MX_BLOCK, mxfp4_dequantize, mxfp4_gemm, mxfp4_grouped_gemm, mxfp4_linear,  # noqa: E402
                  mxfp4_linear_workspace_bytes, mxfp4_pack, mxfp4_packed_sizes, mxfp4_quantize)
 
-EXPORTED += mx.EXPORTED + moe.EXPORTED
+EXPORTED += mx.EXPORTED + moe.EXPORTED + attention.EXPORTED + lora.EXPORTED

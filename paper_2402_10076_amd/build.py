@@ -3,7 +3,7 @@ without a GPU).  quick_gemm.hip is compiled as five translation units in
 parallel (host code and the C ABI; the launches of the stream kernels, the
 tiled kernels, the wave-split kernel and its grouped form), then linked with
 the packing code, the microscaled 4-bit floating-point operators and those of
-mixture-of-experts layers."""
+mixture-of-experts and attention layers."""
 from __future__ import annotations
 
 import os
@@ -30,7 +30,10 @@ UNITS = [("quick_pack.cpp", []),
          ("quick_gemm.hip", ["-DQUICK_PART=4"]),
          ("quick_mx.hip", []),
          ("quick_mx_gemm.hip", []),
-         ("quick_moe.hip", [])]
+         ("quick_moe.hip", []),
+         ("quick_kv4.hip", []),
+         ("quick_attention.hip", []),
+         ("quick_lora.hip", [])]
 
 
 def _msgs(r):

@@ -1,0 +1,607 @@
+// Attention over the paged 4-bit cache.
+#include <algorithm>
+
+#include "quick_attention_plan.h"
+#include "quick_device.h"
+#include "quick_kv4.h"
+
+namespace {
+
+using namespace quick;
+
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+
+// Workgroups of the stream kernel: three for each compute unit.
+constexpr int kStreamWorkers = 768;
+// Pages that a workgroup takes at least: one a wave.
+constexpr int kStreamShare = 4;
+
+// Softmax weights are 2^(s - m), m within a reference of the scores seen so
+// far: set kLift below their largest, and again only when one passes it by
+// kRoom, so that most pages need no exchange between lanes and no rescaling.
+// Weights are then at most 2^kRoom, which f16 holds, and those down to
+// 2^-(24 + kLift) of the largest still count in it.
+constexpr float kLift = 6.0f, kRoom = 14.0f;
+constexpr float kNothing = -3.0e38f;   // a reference before any score
+
+struct AttnArgs {
+    AttnShape s;
+    const uint8_t* q;
+    const uint8_t* cache;
+    const int32_t* table;
+    uint8_t* out;
+    float* lse;
+    float* part;          // [2 * workers][columns][D] sums of a part of an item's pages
+    float* part_ml;       // [2 * workers][columns][2] their references and sums of weights
+    int32_t* joins;       // [workers][8] the item that a worker leaves unfinished
+    int64_t q_token, q_head;
+    int32_t pages, workers;
+    float scale;          // times log2(e)
+};
+
+// Two values of byte BYTE of a word of codes times the scale, as 16-bit pair.
+template <int DT, int BYTE>
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, float scale)
+{
+    if constexpr (DT == QUICK_F16) return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, BYTE));
+    else return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
+}
+template <int DT>
+__device__ __forceinline__ u4_t code_words(uint32_t w, float scale)
+{
+    return u4_t{code_pair<DT, 0>(w, scale), code_pair<DT, 1>(w, scale), code_pair<DT, 2>(w, scale),
+                code_pair<DT, 3>(w, scale)};
+}
+// The scale that byte i of a word of scales stands for.
+__device__ __forceinline__ float scale_of(uint32_t w, int i)
+{
+    return bits_as<float>(i == 3 ? w >> 1 & 0x7F800000u : (i == 2 ? w << 7 : i == 1 ? w << 15 : w << 23) & 0x7F800000u);
+}
+template <int DT>
+__device__ __forceinline__ f4_t mfma16(u4_t a, u4_t b, f4_t c)
+{
+    if constexpr (DT == QUICK_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<h8_t>(a), bits_as<h8_t>(b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<b8_t>(a), bits_as<b8_t>(b), c, 0, 0, 0);
+}
+// Nonzero bits 7, 15, 23, 31 where a byte of scales is beyond the type (its
+// block would be infinite or NaN): above 140 with f16, 252 with bf16.
+template <int DT>
+__device__ __forceinline__ uint32_t beyond(uint32_t w)
+{
+    return ((w & 0x7F7F7F7Fu) + (DT == QUICK_F16 ? 0x73737373u : 0x03030303u)) & w & 0x80808080u;
+}
+
+// Exchanges over the four groups of 16 lanes that share a column.
+template <class F>
+__device__ __forceinline__ float over_groups(float v, F f)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(bits_as<uint32_t>(v), bits_as<uint32_t>(v), false, false);
+    v = f(bits_as<float>(r[0]), bits_as<float>(r[1]));
+    const auto s = __builtin_amdgcn_permlane32_swap(bits_as<uint32_t>(v), bits_as<uint32_t>(v), false, false);
+    return f(bits_as<float>(s[0]), bits_as<float>(s[1]));
+}
+
+// What a lane (group g = lane / 16, c = lane % 16) holds of a page: of the keys
+// of tokens c of each 16, its quarter of the channels; of the values of tokens
+// 4 g .. 4 g + 3 of each 16, channels c * w .. c * w + w - 1 of each 128.
+template <int D>
+struct PageWords {
+    static constexpr int KW = D / 32, HALVES = D > 128 ? 2 : 1, VW = D < 128 ? 2 : 4;
+    uint32_t k[4][KW], ks[HALVES];
+    uint32_t v[HALVES][4][VW], vs[HALVES][4];
+};
+
+template <int D>
+__device__ __forceinline__ void load_page(PageWords<D>& w, const uint8_t* page, int lane)
+{
+    typedef Kv4<D> L;
+    typedef PageWords<D> W;
+    const int c = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint8_t* k = page + L::kKeys + (i * 16 + c) * (D / 2);
+        if constexpr (D == 64) {
+            const u2_t a = *(const u2_t*)(k + g * 8);
+            w.k[i][0] = a[0];
+            w.k[i][1] = a[1];
+        } else {
+#pragma unroll
+            for (int h = 0; h < W::HALVES; h++) {
+                const u4_t a = *(const u4_t*)(k + h * 64 + g * 16);
+#pragma unroll
+                for (int j = 0; j < 4; j++) w.k[i][h * 4 + j] = a[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < W::HALVES; h++) {
+        w.ks[h] = *(const uint32_t*)(page + L::kKeyScales + ((D == 64 ? g >> 1 : g) + 4 * h) * 64 + c * 4);
+        const u4_t s = *(const u4_t*)(page + L::kValueScales + ((D == 64 ? c >> 3 : c >> 2) + 4 * h) * 64 + g * 16);
+#pragma unroll
+        for (int i = 0; i < 4; i++) w.vs[h][i] = s[i];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint8_t* v = page + L::kValues + h * 4096 + ((i * 4 + g) * 16 + c) * (4 * W::VW);
+            if constexpr (D == 64) {
+                const u2_t a = *(const u2_t*)v;
+                w.v[h][i][0] = a[0];
+                w.v[h][i][1] = a[1];
+            } else {
+                const u4_t a = *(const u4_t*)v;
+#pragma unroll
+                for (int j = 0; j < 4; j++) w.v[h][i][j] = a[j];
+            }
+        }
+    }
+}
+
+// Operands of two tiles of 16 channels from the same byte of eight tokens: w
+// holds four tokens of one 16 (a) and of the next (b), eight channels (W == 4)
+// or four of each; the byte's two channels go to the two operands.
+template <int DT, int W, int Y>
+__device__ __forceinline__ void value_words(const uint32_t (&a)[W], const uint32_t (&b)[W], const float (&sa)[4],
+                                            const float (&sb)[4], u4_t& lo, u4_t& hi)
+{
+    uint32_t p[8];
+    if constexpr (W == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            p[e] = code_pair<DT, Y>(a[e], sa[e]);
+            p[4 + e] = code_pair<DT, Y>(b[e], sb[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            p[2 * e] = code_pair<DT, Y>(a[e], sa[2 * e]);
+            p[2 * e + 1] = code_pair<DT, Y + 2>(a[e], sa[2 * e + 1]);
+            p[4 + 2 * e] = code_pair<DT, Y>(b[e], sb[2 * e]);
+            p[5 + 2 * e] = code_pair<DT, Y + 2>(b[e], sb[2 * e + 1]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        lo[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x05040100u);
+        hi[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x07060302u);
+    }
+}
+
+// A column's state: reference, sum of this lane's weights, and the sums of
+// values.  Of d-tile j, register i: channel 128 (j / T) + (4 g + i) T + j % T,
+// T = min(D, 128) / 16.
+template <int D>
+struct Column {
+    float m, l;
+    f4_t o[D / 16];
+};
+
+// Tokens a column sees: lo <= token < hi.
+struct Seen {
+    int lo, hi;
+};
+
+// The blocks of values that are beyond the type make NaN of the columns that
+// see them, and nothing of the others: they are taken out of the product (their
+// scales become 2^-127) and the sums of those columns set.  Seldom run.
+template <int DT, int D>
+__device__ void take_out(PageWords<D>& w, Column<D>& col, Seen seen, int token0, int lane, bool clear)
+{
+    typedef PageWords<D> W;
+    constexpr int TILES = (D < 128 ? D : 128) / 16;
+    const int g = lane >> 4, block = D == 64 ? g >> 1 : g;
+#pragma unroll
+    for (int h = 0; h < W::HALVES; h++) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t mark = beyond<DT>(w.vs[h][i]);
+            for (int e = 0; e < 4; e++) {
+                // lane 16 x + (first lane of a block) has token 16 i + 4 x + e of that block
+                const uint64_t b = __ballot(mark >> (8 * e + 7) & 1);
+                for (int x = 0; x < 4; x++) {
+                    const int token = token0 + 16 * i + 4 * x + e;
+                    bad |= (b >> (16 * x + block * (D == 64 ? 8 : 4)) & 1) && token >= seen.lo && token < seen.hi;
+                }
+            }
+            if (clear) w.vs[h][i] &= ~((mark >> 7) * 0xFFu);
+        }
+        if (bad) {
+#pragma unroll
+            for (int j = 0; j < TILES; j++) col.o[h * TILES + j] = f4_t{NAN, NAN, NAN, NAN};
+        }
+    }
+}
+
+// One page into NC columns of a wave.
+template <int DT, int D, int NC>
+__device__ __forceinline__ void attend(PageWords<D>& w, const u4_t (&q)[NC][D / 32], Column<D> (&col)[NC],
+                                       const Seen (&seen)[NC], int token0, bool masked, float scale, int lane)
+{
+    typedef PageWords<D> W;
+    constexpr int KW = W::KW, TILES = (D < 128 ? D : 128) / 16;
+    const int g = lane >> 4;
+    float p[NC][4][4];
+    {
+        f4_t s[NC][4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+#pragma unroll
+            for (int n = 0; n < NC; n++) s[n][i] = f4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < KW; j++) {
+                const u4_t k = code_words<DT>(w.k[i][j], scale_of(w.ks[j / 4], i));
+#pragma unroll
+                for (int n = 0; n < NC; n++) s[n][i] = mfma16<DT>(k, q[n][j], s[n][i]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NC; n++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) p[n][i][e] = s[n][i][e] * scale;
+    }
+#pragma unroll
+    for (int n = 0; n < NC; n++) {
+        if (masked) {
+            const int lo = seen[n].lo - token0, hi = seen[n].hi - token0;
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int t = 16 * i + 4 * g + e;
+                    p[n][i][e] = t >= lo && t < hi ? p[n][i][e] : -INFINITY;
+                }
+        }
+        float top = p[n][0][0];
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) top = fmaxf(top, p[n][i][e]);
+        if (__ballot(top > col[n].m + kRoom)) {
+            top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
+            const float m = top > col[n].m + kRoom ? top - kLift : col[n].m;
+            const float f = __builtin_amdgcn_exp2f(col[n].m - m);
+            col[n].m = m;
+            col[n].l *= f;
+#pragma unroll
+            for (int j = 0; j < D / 16; j++) col[n].o[j] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                p[n][i][e] = __builtin_amdgcn_exp2f(p[n][i][e] - col[n].m);
+                col[n].l += p[n][i][e];
+            }
+    }
+    uint32_t mark = 0;
+#pragma unroll
+    for (int h = 0; h < W::HALVES; h++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) mark |= beyond<DT>(w.vs[h][i]);
+    if (__ballot(mark != 0)) {
+#pragma unroll
+        for (int n = 0; n < NC; n++) take_out<DT, D>(w, col[n], seen[n], token0, lane, n == NC - 1);
+    }
+#pragma unroll
+    for (int r = 0; r < 2; r++) {
+        u4_t pw[NC];
+#pragma unroll
+        for (int n = 0; n < NC; n++)
+            pw[n] = u4_t{to16x2<DT>(p[n][2 * r][0], p[n][2 * r][1]), to16x2<DT>(p[n][2 * r][2], p[n][2 * r][3]),
+                         to16x2<DT>(p[n][2 * r + 1][0], p[n][2 * r + 1][1]),
+                         to16x2<DT>(p[n][2 * r + 1][2], p[n][2 * r + 1][3])};
+#pragma unroll
+        for (int h = 0; h < W::HALVES; h++) {
+            float sa[4], sb[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                sa[e] = scale_of(w.vs[h][2 * r], e);
+                sb[e] = scale_of(w.vs[h][2 * r + 1], e);
+            }
+            u4_t lo, hi;
+            auto add = [&](int j) {
+#pragma unroll
+                for (int n = 0; n < NC; n++) {
+                    col[n].o[h * TILES + j] = mfma16<DT>(lo, pw[n], col[n].o[h * TILES + j]);
+                    col[n].o[h * TILES + j + 1] = mfma16<DT>(hi, pw[n], col[n].o[h * TILES + j + 1]);
+                }
+            };
+            value_words<DT, W::VW, 0>(w.v[h][2 * r], w.v[h][2 * r + 1], sa, sb, lo, hi);
+            add(0);
+            value_words<DT, W::VW, 1>(w.v[h][2 * r], w.v[h][2 * r + 1], sa, sb, lo, hi);
+            add(2);
+            if constexpr (D != 64) {
+                value_words<DT, W::VW, 2>(w.v[h][2 * r], w.v[h][2 * r + 1], sa, sb, lo, hi);
+                add(4);
+                value_words<DT, W::VW, 3>(w.v[h][2 * r], w.v[h][2 * r + 1], sa, sb, lo, hi);
+                add(6);
+            }
+        }
+    }
+}
+
+// Eight sums of a column to its row of out.
+template <int DT>
+__device__ __forceinline__ u4_t rounded8(const float (&v)[8], float f)
+{
+    return u4_t{to16x2<DT>(v[0] * f, v[1] * f), to16x2<DT>(v[2] * f, v[3] * f), to16x2<DT>(v[4] * f, v[5] * f),
+                to16x2<DT>(v[6] * f, v[7] * f)};
+}
+
+// A few queries of each sequence (16 NC columns, a column being a query and one
+// of the heads that share keys and values).  A wave takes every fourth page of
+// its workgroup's share: scores transposed, keys . queries^T, so that a
+// column's scores are in the lanes that need its weights as the operand of
+// values^T . weights, with no exchange between lanes and nothing in LDS; the
+// waves' sums meet in LDS once an item.
+template <int DT, int D, int NC>
+__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnArgs a)
+{
+    typedef Kv4<D> L;
+    constexpr int BC = 16 * NC, KW = D / 32, TILES = (D < 128 ? D : 128) / 16, ROW = D + 4;
+    __shared__ float sums[4][16][ROW];
+    __shared__ float refs[4][16][2];
+    __shared__ PlanSpace space;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int worker = blockIdx.x;
+    Walk walk = find_share<BC>(a.s, a.workers, worker, kStreamShare, space);
+    int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
+        const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
+        const int take = (int)min((int64_t)(t.cost - walk.page), walk.left);
+        const int p0 = t.p0 + walk.page, p1 = min(p0 + take, t.p1);
+        const int col0 = walk.j * BC;
+        u4_t q[NC][KW];
+        Column<D> col[NC];
+        Seen seen[NC];
+#pragma unroll
+        for (int n = 0; n < NC; n++) {
+            const int cc = col0 + n * 16 + c, i = cc / a.s.group;
+            const bool live = cc < t.columns;
+            const int pos = t.base + i;
+            seen[n].hi = !live ? INT32_MAX : a.s.causal ? min(pos + 1, t.length) : t.length;
+            seen[n].lo = a.s.window && live ? max(0, pos + 1 - a.s.window) : 0;
+            const uint8_t* from = a.q + 2 * ((int64_t)(t.first + i) * a.q_token +
+                                             (int64_t)(walk.h * a.s.group + cc - i * a.s.group) * a.q_head);
+#pragma unroll
+            for (int j = 0; j < KW; j++) {
+                const int piece = D == 64 ? 2 * g + j : 16 * (j / 4) + 4 * g + j % 4;
+                q[n][j] = u4_t{0, 0, 0, 0};
+                if (live) q[n][j] = *(const u4_t*)(from + piece * 16);
+            }
+            col[n].m = kNothing;
+            col[n].l = 0;
+#pragma unroll
+            for (int j = 0; j < D / 16; j++) col[n].o[j] = f4_t{0, 0, 0, 0};
+        }
+        const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
+        int32_t ids = 0;
+        PageWords<D> cur;
+        auto fetch = [&](int n, PageWords<D>& to) {    // page n of this wave
+            if ((n & 63) == 0) ids = table[min(p0 + wave + 4 * (n + lane), p1 - 1)];
+            const int x = __builtin_amdgcn_readlane(ids, n & 63);
+            const bool inside = x >= 0 && x < a.pages;
+            load_page<D>(to, a.cache + ((int64_t)(inside ? x : 0) * a.s.heads + walk.h) * L::kBytes, lane);
+            return inside;
+        };
+        const int count = p1 > p0 + wave ? (p1 - p0 - wave + 3) / 4 : 0;
+        bool ok = false;
+        if (count) ok = fetch(0, cur);
+        for (int n = 0; n < count; n++) {
+            PageWords<D> next;
+            bool next_ok = false;
+            if (n + 1 < count) next_ok = fetch(n + 1, next);
+            const int token0 = (p0 + wave + 4 * n) * kPage;
+            const bool masked = token0 + kPage > t.all_hi || token0 < t.all_lo;
+            if (ok) attend<DT, D, NC>(cur, q, col, seen, token0, masked, a.scale, lane);
+            cur = next;
+            ok = next_ok;
+        }
+        const bool whole = walk.page == 0 && take == t.cost;
+        const int64_t slot = 2 * worker + (first ? 0 : 1);
+        if (walk.page == 0 && !whole) {
+            const int rest = t.cost - take;
+            join[0] = 1 + (int)((rest + walk.share - 1) / walk.share);    // parts
+            join[1] = walk.b;
+            join[2] = walk.j;
+            join[3] = walk.h;
+            join[4] = (int)slot;
+        }
+#pragma unroll
+        for (int n = 0; n < NC; n++) {
+            if (n || !first) __syncthreads();
+            const float l = over_groups(col[n].l, [](float x, float y) { return x + y; });
+            if (g == 0) {
+                refs[wave][c][0] = col[n].m;
+                refs[wave][c][1] = l;
+            }
+#pragma unroll
+            for (int h = 0; h < PageWords<D>::HALVES; h++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    float* to = &sums[wave][c][h * 128 + (4 * g + i) * TILES];
+#pragma unroll
+                    for (int j = 0; j < TILES; j += 4)
+                        *(f4_t*)(to + j) = f4_t{col[n].o[h * TILES + j][i], col[n].o[h * TILES + j + 1][i],
+                                                col[n].o[h * TILES + j + 2][i], col[n].o[h * TILES + j + 3][i]};
+                }
+            __syncthreads();
+            constexpr int PIECES = D / 8;
+            for (int at = threadIdx.x; at < 16 * PIECES; at += 256) {
+                const int x = at / PIECES, d = at % PIECES * 8, cc = col0 + n * 16 + x;
+                if (cc >= t.columns) continue;
+                float m = refs[0][x][0];
+#pragma unroll
+                for (int w = 1; w < 4; w++) m = fmaxf(m, refs[w][x][0]);
+                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0;
+#pragma unroll
+                for (int w = 0; w < 4; w++) {
+                    const float f = __builtin_amdgcn_exp2f(refs[w][x][0] - m);
+                    sum += refs[w][x][1] * f;
+#pragma unroll
+                    for (int j = 0; j < 8; j++) v[j] += sums[w][x][d + j] * f;
+                }
+                if (whole) {
+                    const int i = cc / a.s.group;
+                    const int64_t row = (int64_t)(t.first + i) * (a.s.heads * a.s.group) + walk.h * a.s.group + cc - i * a.s.group;
+                    *(u4_t*)(a.out + 2 * (row * D + d)) = rounded8<DT>(v, sum == 0 ? 0.0f : 1.0f / sum);
+                    if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
+                } else {
+                    float* to = a.part + ((slot * BC + n * 16 + x) * D + d);
+                    *(f4_t*)to = f4_t{v[0], v[1], v[2], v[3]};
+                    *(f4_t*)(to + 4) = f4_t{v[4], v[5], v[6], v[7]};
+                    if (d == 0) {
+                        a.part_ml[(slot * BC + n * 16 + x) * 2] = m;
+                        a.part_ml[(slot * BC + n * 16 + x) * 2 + 1] = sum;
+                    }
+                }
+            }
+        }
+        advance<BC>(a.s, walk, t, take);
+    }
+    if (threadIdx.x < 8) {
+        int v = join[0];
+#pragma unroll
+        for (int i = 1; i < 8; i++) v = threadIdx.x == i ? join[i] : v;
+        a.joins[worker * 8 + threadIdx.x] = v;
+    }
+}
+
+// Joins the parts of the item that a worker left unfinished: its own, and the
+// first ones of the workers after it.  A thread has eight channels of a column.
+template <int DT, int D, int BC>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+{
+    const int worker = blockIdx.x;
+    const int parts = a.joins[worker * 8];
+    if (parts == 0) return;
+    const int b = a.joins[worker * 8 + 1], j = a.joins[worker * 8 + 2], h = a.joins[worker * 8 + 3];
+    const int64_t slot0 = a.joins[worker * 8 + 4];
+    const Tile t = tile_of<BC>(a.s, b, j);
+    constexpr int PIECES = D / 8;
+    for (int at = threadIdx.x + 256 * blockIdx.y; at < BC * PIECES; at += 256 * gridDim.y) {
+        const int x = at / PIECES, d = at % PIECES * 8, cc = j * BC + x;
+        if (cc >= t.columns) continue;
+        float m = kNothing, sum = 0, v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int i = 0; i < parts; i++) {
+            const int64_t slot = i == 0 ? slot0 : 2 * (int64_t)(worker + i);
+            const float* ml = a.part_ml + (slot * BC + x) * 2;
+            const f4_t* from = (const f4_t*)(a.part + ((slot * BC + x) * D + d));
+            const f4_t p = from[0], r = from[1];
+            const float n = fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - n), e = __builtin_amdgcn_exp2f(ml[0] - n);
+            m = n;
+            sum = sum * f + ml[1] * e;
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                v[k] = v[k] * f + p[k] * e;
+                v[4 + k] = v[4 + k] * f + r[k] * e;
+            }
+        }
+        const int i = cc / a.s.group;
+        const int64_t row = (int64_t)(t.first + i) * (a.s.heads * a.s.group) + h * a.s.group + cc - i * a.s.group;
+        *(u4_t*)(a.out + 2 * (row * D + d)) = rounded8<DT>(v, sum == 0 ? 0.0f : 1.0f / sum);
+        if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
+// Columns of a workgroup's tile.
+int columns_of(const quick_attention_t& a)
+{
+    return a.most * (a.q_heads / a.heads) <= 16 ? 16 : 32;
+}
+
+int workers_of(const quick_attention_t& a)
+{
+    // no more than there can be pages of items
+    const int64_t group = a.q_heads / a.heads, bc = columns_of(a);
+    const int64_t rows = std::min(a.T, a.seqs * std::min(a.most, a.T));
+    const int64_t items = (std::min(a.seqs, a.T) + rows * group / bc + 1) * a.heads;
+    const int64_t share = std::max<int64_t>(1, (a.table_width + kStreamShare - 1) / kStreamShare);
+    return (int)std::min<int64_t>(kStreamWorkers, items > kStreamWorkers / share ? kStreamWorkers : items * share);
+}
+
+template <int DT, int D, int NC>
+void launch_attention(const AttnArgs& a, hipStream_t hs)
+{
+    attn_stream_kernel<DT, D, NC><<<a.workers, 256, 0, hs>>>(a);
+    attn_join_kernel<DT, D, 16 * NC><<<a.workers, 256, 0, hs>>>(a);
+}
+template <int DT>
+void launch_attention(const AttnArgs& a, int64_t D, int columns, hipStream_t hs)
+{
+#define QUICK_ATTN(D) (columns == 16 ? launch_attention<DT, D, 1>(a, hs) : launch_attention<DT, D, 2>(a, hs))
+    if (D == 64) QUICK_ATTN(64);
+    else if (D == 128) QUICK_ATTN(128);
+    else QUICK_ATTN(256);
+#undef QUICK_ATTN
+}
+
+int check_attention(const quick_attention_t& a)
+{
+    if (a.T < 0 || a.T >= (1 << 24) || a.heads < 1 || a.heads > QUICK_KV4_MAX_HEADS || a.q_heads < a.heads ||
+        a.q_heads % a.heads != 0 || a.q_heads / a.heads > 64 || a.pages < 1 || a.pages >= (1 << 25) || a.seqs < 0 ||
+        a.seqs > QUICK_KV4_MAX_SEQS || a.table_width < 0 || a.table_width >= (1 << 24) || a.most < 1 || a.window < 0 ||
+        (a.window && !a.causal) || a.q_token < 0 || a.q_head < 0 || a.q_token >= ((int64_t)1 << 40) ||
+        a.q_head >= ((int64_t)1 << 40))
+        return QUICK_ERR_SHAPE;
+    if (a.D != 64 && a.D != 128 && a.D != 256) return QUICK_ERR_UNSUPPORTED;
+    if (a.T * a.q_heads * a.D >= ((int64_t)1 << 40)) return QUICK_ERR_SHAPE;
+    return QUICK_OK;
+}
+
+}  // namespace
+
+extern "C" size_t quick_kv4_attention_workspace_bytes(const quick_attention_t* p)
+{
+    if (!p || check_attention(*p) || p->T == 0 || p->seqs == 0) return 0;
+    const size_t w = (size_t)workers_of(*p), c = (size_t)columns_of(*p);
+    return w * 32 + 2 * w * c * ((size_t)p->D + 2) * sizeof(float);
+}
+
+extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, int dtype, const void* cache, const int32_t* table,
+                                   const int32_t* lengths, const int32_t* offsets, void* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, void* stream)
+{
+    if (!p || (dtype != QUICK_F16 && dtype != QUICK_BF16)) return QUICK_ERR_INVALID_ARG;
+    const int st = check_attention(*p);
+    if (st) return st;
+    if (p->T == 0 || p->seqs == 0) return QUICK_OK;
+    if (!q || !cache || !lengths || !out || (p->table_width && !table)) return QUICK_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(cache, 16) || !aligned(out, 16) || !aligned(table, 4) || !aligned(lengths, 4) ||
+        !aligned(offsets, 4) || !aligned(lse, 4) || p->q_token % 8 || p->q_head % 8)
+        return QUICK_ERR_ALIGNMENT;
+    const size_t need = quick_kv4_attention_workspace_bytes(p);
+    if (!workspace || workspace_bytes < need) return QUICK_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return QUICK_ERR_ALIGNMENT;
+    AttnArgs a{};
+    a.workers = workers_of(*p);
+    const int columns = columns_of(*p);
+    a.s.lengths = lengths;
+    a.s.offsets = offsets;
+    a.s.T = (int32_t)p->T;
+    a.s.heads = (int32_t)p->heads;
+    a.s.group = (int32_t)(p->q_heads / p->heads);
+    a.s.seqs = (int32_t)p->seqs;
+    a.s.width = (int32_t)p->table_width;
+    a.s.most = (int32_t)std::min<int64_t>(p->most, p->T);
+    a.s.window = (int32_t)std::min<int64_t>(p->window, INT32_MAX);
+    a.s.causal = p->causal != 0;
+    a.q = (const uint8_t*)q;
+    a.cache = (const uint8_t*)cache;
+    a.table = table;
+    a.out = (uint8_t*)out;
+    a.lse = lse;
+    a.joins = (int32_t*)workspace;
+    a.part = (float*)((uint8_t*)workspace + (size_t)a.workers * 32);
+    a.part_ml = a.part + 2 * (size_t)a.workers * columns * p->D;
+    a.q_token = p->q_token;
+    a.q_head = p->q_head;
+    a.pages = (int32_t)p->pages;
+    a.scale = p->scale * 1.44269504088896341f;
+    (void)hipGetLastError();
+    if (dtype == QUICK_F16) launch_attention<QUICK_F16>(a, p->D, columns, (hipStream_t)stream);
+    else launch_attention<QUICK_BF16>(a, p->D, columns, (hipStream_t)stream);
+    return launched();
+}

@@ -1,0 +1,258 @@
+"""Attention over the paged 4-bit cache (include/quick_attention.h) on the GPU
+against the binary64 form."""
+import math
+
+import pytest
+import torch
+
+import attn_util as A
+import paper_2402_10076_amd as Q
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+
+class Batch:
+    """Sequences in a cache of shuffled pages, slots of no token filled with bytes that must not count."""
+
+    def __init__(self, seed, lengths, new, heads, group, D, dtype, spare=1, width=None, kscale=1.0, fill=0xFF):
+        g = A.gen(seed, len(lengths), heads, group, D)
+        self.lengths, self.new, self.group, self.dtype = lengths, new, group, A.TYPES[dtype]
+        need = [-(-n // 64) for n in lengths]
+        pages = sum(need) + spare
+        width = max(need + [1]) + 1 if width is None else width
+        ids = torch.randperm(pages, generator=g)
+        self.table = torch.full((len(lengths), width), pages + 7, dtype=torch.int32)
+        self.cache = Q.kv4_cache(pages, heads, D).fill_(fill)
+        self.k, self.v = [], []
+        at = 0
+        for b, n in enumerate(lengths):
+            self.table[b, :need[b]] = ids[at:at + need[b]]
+            at += need[b]
+            k, v = (A.normal(g, n, heads, D, scale=s, dtype=self.dtype) for s in (kscale, 1.0))
+            t = torch.arange(n)
+            slots = (self.table[b, t // 64].long() * 64 + t % 64).to(torch.int32) if n else t.to(torch.int32)
+            Q.kv4_write(self.cache, k.cuda(), v.cuda(), slots.cuda())
+            self.k.append(A.rounded(k))
+            self.v.append(A.rounded(v))
+        self.offsets = [0]
+        for n in new:
+            self.offsets.append(self.offsets[-1] + n)
+        self.q = A.normal(g, self.offsets[-1], heads * group, D, scale=1.5, dtype=self.dtype)
+
+    def args(self):
+        return (self.q.cuda(), self.cache, self.table.cuda(), torch.tensor(self.lengths, dtype=torch.int32).cuda())
+
+    def run(self, **kw):
+        if "offsets" not in kw:
+            kw["offsets"] = torch.tensor(self.offsets, dtype=torch.int32).cuda()
+        lse = torch.full(self.q.shape[:2], 7.0, device="cuda")
+        kw.setdefault("most", max(self.new + [1]))
+        return Q.kv4_attention(*self.args(), lse=lse, **kw), lse
+
+    def check(self, **kw):
+        ref = {n: kw[n] for n in ("scale", "window", "causal") if n in kw}
+        out, lse = self.run(**kw)
+        want, want_lse, tol = A.attention(self.q.double(), self.k, self.v, self.lengths, self.offsets, self.group,
+                                          self.dtype, **ref)
+        err = (out.cpu().double() - want).abs()
+        assert bool((err <= tol).all()), "err %.3g, of the bound %.3g" % (float(err.max()), float((err / tol).max()))
+        got = lse.cpu().double()
+        empty = want_lse == -math.inf
+        assert torch.equal(got == -math.inf, empty)
+        assert not out.cpu()[empty].any()
+        # scores of up to a few tens, off by the bound of a weight; the logarithm's last places
+        assert float((got - want_lse)[~empty].abs().max() if bool((~empty).any()) else 0) <= 2e-4
+        return out
+
+
+LENGTHS = [[1], [2, 0, 63], [64], [65, 1, 200], [127, 128, 129], [1000], [300, 5, 64, 0, 777, 63]]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,group,D", [(1, 1, 64), (2, 4, 128), (3, 5, 64), (2, 1, 128), (1, 16, 256), (2, 3, 256),
+                                           (8, 8, 128), (1, 32, 128)])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=lambda v: "-".join(map(str, v)))
+def test_single_tokens(lengths, heads, group, D, dtype):
+    say("decode", lengths, heads, group, D, dtype)
+    b = Batch(1, lengths, [1] * len(lengths), heads, group, D, dtype)
+    b.check(offsets=None)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lengths,new,heads,group,D", [
+    ([70, 9, 300], [5, 5, 5], 2, 4, 128), ([70, 9, 300], [3, 0, 7], 2, 2, 64), ([100, 64, 65], [1, 64, 33], 1, 4, 128),
+    ([500], [500], 2, 1, 64), ([200, 1, 130], [150, 1, 130], 1, 8, 128), ([333, 40], [77, 40], 1, 3, 256),
+    ([260, 2], [129, 2], 4, 2, 128), ([64, 64], [64, 1], 1, 1, 256), ([5, 600], [5, 2], 1, 64, 64),
+    ([400], [300], 1, 5, 128), ([1100, 90], [700, 3], 2, 4, 64)])
+def test_prompts_and_drafts(lengths, new, heads, group, D, dtype):
+    say("prompts", lengths, new, heads, group, D, dtype)
+    b = Batch(2, lengths, new, heads, group, D, dtype)
+    out = b.check()
+    b.check(causal=False)
+    b.check(window=37, scale=-0.2)
+    b.check(window=1)
+    b.check(window=100000)
+    # without `most`
+    again, _ = b.run(most=None)
+    assert torch.allclose(again.float(), out.float(), rtol=0.03, atol=0.03)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 3, 90])
+def test_more_queries_than_tokens(new, dtype):
+    """Queries that stand before the first token see nothing: zeros, and a logarithm of -inf."""
+    b = Batch(3, [0, 2, 70, 1], [new] * 4, 2, 4, 128, dtype)
+    b.check()
+    b.check(window=2)
+    b.check(causal=False)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_large_and_equal_scores(dtype):
+    """Scores of hundreds, rising and falling along the sequence, and all equal."""
+    b = Batch(4, [700, 130], [4, 130], 2, 4, 128, dtype, kscale=12.0)
+    b.check(scale=0.5)
+    b.check(scale=-0.5)
+    b.check(scale=0.0)
+
+
+@pytest.mark.parametrize("D,new", [(64, 1), (128, 1), (256, 1), (64, 40), (128, 40), (256, 40)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_nan_and_infinity_where_nothing_looks(dtype, D, new):
+    """NaN keys and values of a token enter the rows that see it and no others, whatever the slots behind the last
+    token hold (0xFF: scales of NaN)."""
+    lengths, T = [100, 64 * 3], [min(new, 100), new]
+    b = Batch(5, lengths, T, 2, 4, D, dtype)
+    for bad, token in ((0, 99), (1, 150)):
+        # a later token's NaN: rows before it are as without it
+        for window in (0, 20):
+            ref, _ = b.run(window=window)
+            k, v = (torch.zeros(1, 2, D, dtype=b.dtype) for _ in range(2))
+            v[0, 0, 1] = float("nan")
+            k[0, 1, D - 1] = float("inf")
+            slot = (b.table[bad, token // 64] * 64 + token % 64).view(1).cuda()
+            kept = b.cache.clone()
+            Q.kv4_write(b.cache, k.cuda(), v.cuda(), slot)
+            out, _ = b.run(window=window)
+            b.cache.copy_(kept)
+            first = b.lengths[bad] - T[bad]
+            for s in range(2):
+                for i in range(T[s]):
+                    row = b.offsets[s] + i
+                    pos = b.lengths[s] - T[s] + i
+                    sees = s == bad and pos >= token and (not window or token > pos - window)
+                    got, want = out[row].cpu(), ref[row].cpu()
+                    if not sees:
+                        assert torch.equal(got, want), (s, i, pos, token, window)
+                    else:
+                        assert got[:4, :32].isnan().all() and not got[:4, 32:].isnan().any()   # the block of head 0
+                        assert got[4:].isnan().all()                                          # a NaN score of head 1
+            assert first >= 0
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_pages_outside_the_cache(new):
+    """Their tokens are not seen, whichever page of the sequence it is."""
+    b = Batch(6, [400, 300], [new, new], 2, 4, 128, "f16")
+    for page, bad in ((0, -1), (2, 1 << 24), (6, -(1 << 31)), (4, b.cache.shape[0])):
+        table = b.table.clone()
+        table[0, page] = bad
+        known = [torch.arange(n) // 64 != (page if i == 0 else -1) for i, n in enumerate(b.lengths)]
+        q, cache, _, lengths = b.args()
+        out = Q.kv4_attention(q, cache, table.cuda(), lengths, offsets=torch.tensor(b.offsets, dtype=torch.int32).cuda(), most=new)
+        want, _, tol = A.attention(b.q.double(), b.k, b.v, b.lengths, b.offsets, b.group, b.dtype, known=known)
+        assert bool(((out.cpu().double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("most", [3, 60])
+def test_rows_of_no_sequence_and_broken_offsets(most):
+    """Rows that belong to no sequence keep their values; offsets and lengths out of range are clamped."""
+    b = Batch(7, [100, 90, 80], [2, 3, 1], 2, 2, 64, "bf16")
+    q = torch.cat([A.normal(A.gen(8), 2, 4, 64, dtype=torch.bfloat16), b.q, A.normal(A.gen(9), 5, 4, 64, dtype=torch.bfloat16)]).cuda()
+    out = torch.full_like(q, 5.0)
+    _, cache, table, lengths = b.args()
+    o = torch.tensor([x + 2 for x in b.offsets], dtype=torch.int32).cuda()
+    Q.kv4_attention(q, cache, table, lengths, offsets=o, most=most, out=out)
+    ref, _ = b.run()
+    assert torch.equal(out[2:8], ref) and bool((out[:2] == 5).all()) and bool((out[8:] == 5).all())
+    for broken in ([-5, 2, 1 << 30, 7], [9, 3, 2, -1], [1 << 30] * 4, [-(1 << 31)] * 4, [0, 11, 11, 11]):
+        Q.kv4_attention(q, cache, table, lengths, offsets=torch.tensor(broken, dtype=torch.int32).cuda(), most=most)
+    for n in ([-1, 1 << 30, 64 * table.shape[1] + 1], [-(1 << 31), (1 << 31) - 1, 0]):
+        y = Q.kv4_attention(q, cache, table, torch.tensor(n, dtype=torch.int32).cuda(), offsets=o, most=most)
+        assert not y[2:4].any()
+    torch.cuda.synchronize()
+
+
+def test_most_bounds_the_rows():
+    """Of a sequence with more queries than `most` so many of the first are worked on, at their own positions."""
+    b = Batch(10, [200, 100], [20, 4], 2, 4, 128, "f16")
+    ref, _ = b.run()
+    out = torch.full_like(ref, 3.0)
+    b.run(most=4, out=out)
+    assert torch.allclose(out[:4].float(), ref[:4].float(), atol=2e-3) and bool((out[4:20] == 3).all())
+    assert torch.allclose(out[20:].float(), ref[20:].float(), atol=2e-3)
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_strided_queries(new):
+    """Heads of a projection's output, and heads outermost: the bits of the contiguous call."""
+    b = Batch(11, [150, 97], [new, new], 2, 4, 128, "f16")
+    ref, _ = b.run()
+    T = b.q.shape[0]
+    wide = torch.zeros((T, 12, 128), dtype=torch.float16)
+    wide[:, 2:10] = b.q
+    for q in (wide.cuda()[:, 2:10], b.q.transpose(0, 1).contiguous().cuda().transpose(0, 1)):
+        _, cache, table, lengths = b.args()
+        assert torch.equal(Q.kv4_attention(q, cache, table, lengths, offsets=torch.tensor(b.offsets, dtype=torch.int32).cuda(), most=new), ref)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_many_sequences(dtype):
+    """More sequences than threads plan, some without queries or tokens."""
+    g = A.gen(12)
+    lengths = torch.randint(0, 90, (600,), generator=g).tolist()
+    new = [min(n, int(x)) for n, x in zip(lengths, torch.randint(0, 3, (600,), generator=g))]
+    Batch(12, lengths, new, 1, 2, 64, dtype).check()
+    Batch(13, lengths[:300], [1] * 300, 1, 2, 64, dtype).check(offsets=None)
+
+
+def test_long_sequence_is_shared_out():
+    """A sequence over many workgroups, beside short ones, twice the same."""
+    b = Batch(14, [20000, 3, 64], [1, 1, 1], 2, 4, 128, "bf16")
+    out = b.check(offsets=None)
+    assert torch.equal(b.run(offsets=None)[0], out)
+    b = Batch(15, [9000, 70], [40, 70], 1, 4, 64, "f16")
+    out = b.check()
+    assert torch.equal(b.run()[0], out)
+
+
+def test_window_far_behind():
+    """Most of the pages are outside the window: they are not read (their ids are not valid)."""
+    b = Batch(16, [5000, 900], [6, 1], 2, 4, 128, "f16")
+    b.table[0, :(5000 - 6 - 100) // 64] = -1
+    b.check(window=100)
+
+
+def test_cache_past_32_bits():
+    """Pages beyond 4 GiB."""
+    b = Batch(17, [130], [1], 8, 1, 256, "f16")
+    page = b.cache[0].numel()
+    pages = (1 << 32) // page + 4
+    far = torch.empty((pages, *b.cache.shape[1:]), dtype=torch.uint8, device="cuda")
+    n = b.cache.shape[0]
+    far[-n:] = b.cache
+    ref, _ = b.run(offsets=None)
+    q, _, table, lengths = b.args()
+    assert torch.equal(Q.kv4_attention(q, far, table + (pages - n), lengths), ref)
+
+
+def test_nothing_to_do():
+    cache = Q.kv4_cache(1, 2, 64)
+    i = torch.zeros(0, dtype=torch.int32, device="cuda")
+    q = torch.empty((0, 4, 64), dtype=torch.float16, device="cuda")
+    assert Q.kv4_attention(q, cache, i.view(0, 3), i).shape == (0, 4, 64)
+    # a table without pages: every row sees nothing
+    q = torch.ones((2, 4, 64), dtype=torch.float16, device="cuda")
+    two = torch.tensor([5, 0], dtype=torch.int32, device="cuda")
+    assert not Q.kv4_attention(q, cache, torch.zeros((2, 0), dtype=torch.int32, device="cuda"), two).any()
