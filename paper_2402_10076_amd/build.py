@@ -33,6 +33,7 @@ UNITS = [("quick_pack.cpp", []),
          ("quick_moe.hip", []),
          ("quick_kv4.hip", []),
          ("quick_attention.hip", []),
+         ("quick_attention_tiled.hip", []),
          ("quick_lora.hip", [])]
 
 

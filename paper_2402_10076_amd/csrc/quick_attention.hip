@@ -1,76 +1,17 @@
 // Attention over the paged 4-bit cache.
 #include <algorithm>
+#include <cmath>
 
-#include "quick_attention_plan.h"
-#include "quick_device.h"
-#include "quick_kv4.h"
+#include "quick_attention_parts.h"
 
 namespace {
 
 using namespace quick;
 
-typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
-
 // Workgroups of the stream kernel: three for each compute unit.
 constexpr int kStreamWorkers = 768;
-// Pages that a workgroup takes at least: one a wave.
-constexpr int kStreamShare = 4;
-
-// Softmax weights are 2^(s - m), m within a reference of the scores seen so
-// far: set kLift below their largest, and again only when one passes it by
-// kRoom, so that most pages need no exchange between lanes and no rescaling.
-// Weights are then at most 2^kRoom, which f16 holds, and those down to
-// 2^-(24 + kLift) of the largest still count in it.
-constexpr float kLift = 6.0f, kRoom = 14.0f;
-constexpr float kNothing = -3.0e38f;   // a reference before any score
-
-struct AttnArgs {
-    AttnShape s;
-    const uint8_t* q;
-    const uint8_t* cache;
-    const int32_t* table;
-    uint8_t* out;
-    float* lse;
-    float* part;          // [2 * workers][columns][D] sums of a part of an item's pages
-    float* part_ml;       // [2 * workers][columns][2] their references and sums of weights
-    int32_t* joins;       // [workers][8] the item that a worker leaves unfinished
-    int64_t q_token, q_head;
-    int32_t pages, workers;
-    float scale;          // times log2(e)
-};
-
-// Two values of byte BYTE of a word of codes times the scale, as 16-bit pair.
-template <int DT, int BYTE>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, float scale)
-{
-    if constexpr (DT == QUICK_F16) return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, BYTE));
-    else return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
-}
-template <int DT>
-__device__ __forceinline__ u4_t code_words(uint32_t w, float scale)
-{
-    return u4_t{code_pair<DT, 0>(w, scale), code_pair<DT, 1>(w, scale), code_pair<DT, 2>(w, scale),
-                code_pair<DT, 3>(w, scale)};
-}
-// The scale that byte i of a word of scales stands for.
-__device__ __forceinline__ float scale_of(uint32_t w, int i)
-{
-    return bits_as<float>(i == 3 ? w >> 1 & 0x7F800000u : (i == 2 ? w << 7 : i == 1 ? w << 15 : w << 23) & 0x7F800000u);
-}
-template <int DT>
-__device__ __forceinline__ f4_t mfma16(u4_t a, u4_t b, f4_t c)
-{
-    if constexpr (DT == QUICK_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<h8_t>(a), bits_as<h8_t>(b), c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<b8_t>(a), bits_as<b8_t>(b), c, 0, 0, 0);
-}
-// Nonzero bits 7, 15, 23, 31 where a byte of scales is beyond the type (its
-// block would be infinite or NaN): above 140 with f16, 252 with bf16.
-template <int DT>
-__device__ __forceinline__ uint32_t beyond(uint32_t w)
-{
-    return ((w & 0x7F7F7F7Fu) + (DT == QUICK_F16 ? 0x73737373u : 0x03030303u)) & w & 0x80808080u;
-}
+// What a workgroup takes at least, and what an item costs beside its pages.
+constexpr int kStreamShare = 8, kStreamStart = 4;
 
 // Exchanges over the four groups of 16 lanes that share a column.
 template <class F>
@@ -133,36 +74,6 @@ __device__ __forceinline__ void load_page(PageWords<D>& w, const uint8_t* page, 
                 for (int j = 0; j < 4; j++) w.v[h][i][j] = a[j];
             }
         }
-    }
-}
-
-// Operands of two tiles of 16 channels from the same byte of eight tokens: w
-// holds four tokens of one 16 (a) and of the next (b), eight channels (W == 4)
-// or four of each; the byte's two channels go to the two operands.
-template <int DT, int W, int Y>
-__device__ __forceinline__ void value_words(const uint32_t (&a)[W], const uint32_t (&b)[W], const float (&sa)[4],
-                                            const float (&sb)[4], u4_t& lo, u4_t& hi)
-{
-    uint32_t p[8];
-    if constexpr (W == 4) {
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            p[e] = code_pair<DT, Y>(a[e], sa[e]);
-            p[4 + e] = code_pair<DT, Y>(b[e], sb[e]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-            p[2 * e] = code_pair<DT, Y>(a[e], sa[2 * e]);
-            p[2 * e + 1] = code_pair<DT, Y + 2>(a[e], sa[2 * e + 1]);
-            p[4 + 2 * e] = code_pair<DT, Y>(b[e], sb[2 * e]);
-            p[5 + 2 * e] = code_pair<DT, Y + 2>(b[e], sb[2 * e + 1]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        lo[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x05040100u);
-        hi[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x07060302u);
     }
 }
 
@@ -322,14 +233,6 @@ __device__ __forceinline__ void attend(PageWords<D>& w, const u4_t (&q)[NC][D / 
     }
 }
 
-// Eight sums of a column to its row of out.
-template <int DT>
-__device__ __forceinline__ u4_t rounded8(const float (&v)[8], float f)
-{
-    return u4_t{to16x2<DT>(v[0] * f, v[1] * f), to16x2<DT>(v[2] * f, v[3] * f), to16x2<DT>(v[4] * f, v[5] * f),
-                to16x2<DT>(v[6] * f, v[7] * f)};
-}
-
 // A few queries of each sequence (16 NC columns, a column being a query and one
 // of the heads that share keys and values).  A wave takes every fourth page of
 // its workgroup's share: scores transposed, keys . queries^T, so that a
@@ -350,8 +253,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
     int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
         const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
-        const int take = (int)min((int64_t)(t.cost - walk.page), walk.left);
-        const int p0 = t.p0 + walk.page, p1 = min(p0 + take, t.p1);
+        const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
+        int p0, p1;
+        pages_of(a.s, t, walk.at, take, p0, p1);
         const int col0 = walk.j * BC;
         u4_t q[NC][KW];
         Column<D> col[NC];
@@ -369,7 +273,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
             for (int j = 0; j < KW; j++) {
                 const int piece = D == 64 ? 2 * g + j : 16 * (j / 4) + 4 * g + j % 4;
                 q[n][j] = u4_t{0, 0, 0, 0};
-                if (live) q[n][j] = *(const u4_t*)(from + piece * 16);
+                if (live) q[n][j] = *(const u4_t*)(from + piece * 16) ^ a.q_sign;
             }
             col[n].m = kNothing;
             col[n].l = 0;
@@ -399,9 +303,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
             cur = next;
             ok = next_ok;
         }
-        const bool whole = walk.page == 0 && take == t.cost;
+        const bool whole = walk.at == 0 && take == t.cost;
         const int64_t slot = 2 * worker + (first ? 0 : 1);
-        if (walk.page == 0 && !whole) {
+        if (walk.at == 0 && !whole) {
             const int rest = t.cost - take;
             join[0] = 1 + (int)((rest + walk.share - 1) / walk.share);    // parts
             join[1] = walk.b;
@@ -509,7 +413,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 // Columns of a workgroup's tile.
 int columns_of(const quick_attention_t& a)
 {
-    return a.most * (a.q_heads / a.heads) <= 16 ? 16 : 32;
+    const int64_t n = a.most * (a.q_heads / a.heads);
+    return n <= 16 ? 16 : n <= 32 ? 32 : kTiledColumns;
 }
 
 int workers_of(const quick_attention_t& a)
@@ -518,24 +423,32 @@ int workers_of(const quick_attention_t& a)
     const int64_t group = a.q_heads / a.heads, bc = columns_of(a);
     const int64_t rows = std::min(a.T, a.seqs * std::min(a.most, a.T));
     const int64_t items = (std::min(a.seqs, a.T) + rows * group / bc + 1) * a.heads;
-    const int64_t share = std::max<int64_t>(1, (a.table_width + kStreamShare - 1) / kStreamShare);
-    return (int)std::min<int64_t>(kStreamWorkers, items > kStreamWorkers / share ? kStreamWorkers : items * share);
+    const int64_t least = bc == kTiledColumns ? kTiledShare : kStreamShare;
+    const int64_t most = bc == kTiledColumns ? kTiledWorkers : kStreamWorkers;
+    const int64_t shares = std::max<int64_t>(1, (a.table_width + least - 1) / least);
+    return (int)(items > most / shares ? most : items * shares);
 }
 
-template <int DT, int D, int NC>
-void launch_attention(const AttnArgs& a, hipStream_t hs)
+template <int DT, int D>
+void launch_attention(const AttnArgs& a, int columns, hipStream_t hs)
 {
-    attn_stream_kernel<DT, D, NC><<<a.workers, 256, 0, hs>>>(a);
-    attn_join_kernel<DT, D, 16 * NC><<<a.workers, 256, 0, hs>>>(a);
+    if (columns == 16) {
+        attn_stream_kernel<DT, D, 1><<<a.workers, 256, 0, hs>>>(a);
+        attn_join_kernel<DT, D, 16><<<a.workers, 256, 0, hs>>>(a);
+    } else if (columns == 32) {
+        attn_stream_kernel<DT, D, 2><<<a.workers, 256, 0, hs>>>(a);
+        attn_join_kernel<DT, D, 32><<<a.workers, 256, 0, hs>>>(a);
+    } else {
+        launch_tiled_attention(a, DT, D, hs);
+        attn_join_kernel<DT, D, kTiledColumns><<<dim3(a.workers, kTiledColumns * D / 2048), 256, 0, hs>>>(a);
+    }
 }
 template <int DT>
 void launch_attention(const AttnArgs& a, int64_t D, int columns, hipStream_t hs)
 {
-#define QUICK_ATTN(D) (columns == 16 ? launch_attention<DT, D, 1>(a, hs) : launch_attention<DT, D, 2>(a, hs))
-    if (D == 64) QUICK_ATTN(64);
-    else if (D == 128) QUICK_ATTN(128);
-    else QUICK_ATTN(256);
-#undef QUICK_ATTN
+    if (D == 64) launch_attention<DT, 64>(a, columns, hs);
+    else if (D == 128) launch_attention<DT, 128>(a, columns, hs);
+    else launch_attention<DT, 256>(a, columns, hs);
 }
 
 int check_attention(const quick_attention_t& a)
@@ -588,6 +501,7 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
     a.s.most = (int32_t)std::min<int64_t>(p->most, p->T);
     a.s.window = (int32_t)std::min<int64_t>(p->window, INT32_MAX);
     a.s.causal = p->causal != 0;
+    a.s.start = columns == kTiledColumns ? kTiledStart : kStreamStart;
     a.q = (const uint8_t*)q;
     a.cache = (const uint8_t*)cache;
     a.table = table;
@@ -599,7 +513,9 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
     a.q_token = p->q_token;
     a.q_head = p->q_head;
     a.pages = (int32_t)p->pages;
-    a.scale = p->scale * 1.44269504088896341f;
+    // (never zero: a hidden score is -infinity times it)
+    a.scale = std::max(std::fabs(p->scale) * 1.44269504088896341f, 1e-30f);
+    a.q_sign = p->scale < 0 ? 0x80008000u : 0;
     (void)hipGetLastError();
     if (dtype == QUICK_F16) launch_attention<QUICK_F16>(a, p->D, columns, (hipStream_t)stream);
     else launch_attention<QUICK_BF16>(a, p->D, columns, (hipStream_t)stream);

@@ -1,0 +1,113 @@
+// What the kernels of quick_attention.hip and quick_attention_tiled.hip share:
+// arguments, the softmax's reference, and codes as operands.
+#pragma once
+#include "quick_attention_plan.h"
+#include "quick_device.h"
+#include "quick_kv4.h"
+
+namespace quick {
+
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+typedef float f16_t __attribute__((ext_vector_type(16)));
+
+// Softmax weights are 2^(s - m), m within a reference of the scores seen so
+// far: set kLift below their largest, and again only when one passes it by
+// kRoom, so that most pages need no exchange between lanes and no rescaling.
+// Weights are then at most 2^kRoom, which f16 holds, and those down to
+// 2^-(24 + kLift) of the largest still count in it.
+constexpr float kLift = 6.0f, kRoom = 14.0f;
+constexpr float kNothing = -3.0e38f;   // a reference before any score
+
+struct AttnArgs {
+    AttnShape s;
+    const uint8_t* q;
+    const uint8_t* cache;
+    const int32_t* table;
+    uint8_t* out;
+    float* lse;
+    float* part;          // [2 * workers][columns][D] sums of a part of an item's pages
+    float* part_ml;       // [2 * workers][columns][2] their references and sums of weights
+    int32_t* joins;       // [workers][8] the item that a worker leaves unfinished
+    int64_t q_token, q_head;
+    int32_t pages, workers;
+    float scale;          // of the scores times log2(e), without its sign
+    uint32_t q_sign;      // changes q's sign where the scale is negative
+};
+
+// Two values of byte BYTE of a word of codes times the scale, as 16-bit pair.
+template <int DT, int BYTE>
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, float scale)
+{
+    if constexpr (DT == QUICK_F16) return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, BYTE));
+    else return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
+}
+template <int DT>
+__device__ __forceinline__ u4_t code_words(uint32_t w, float scale)
+{
+    return u4_t{code_pair<DT, 0>(w, scale), code_pair<DT, 1>(w, scale), code_pair<DT, 2>(w, scale),
+                code_pair<DT, 3>(w, scale)};
+}
+// The scale that byte i of a word of scales stands for.
+__device__ __forceinline__ float scale_of(uint32_t w, int i)
+{
+    return bits_as<float>(i == 3 ? w >> 1 & 0x7F800000u : (i == 2 ? w << 7 : i == 1 ? w << 15 : w << 23) & 0x7F800000u);
+}
+template <int DT>
+__device__ __forceinline__ f4_t mfma16(u4_t a, u4_t b, f4_t c)
+{
+    if constexpr (DT == QUICK_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<h8_t>(a), bits_as<h8_t>(b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<b8_t>(a), bits_as<b8_t>(b), c, 0, 0, 0);
+}
+// Nonzero bits 7, 15, 23, 31 where a byte of scales is beyond the type (its
+// block would be infinite or NaN): above 140 with f16, 252 with bf16.
+template <int DT>
+__device__ __forceinline__ uint32_t beyond(uint32_t w)
+{
+    return ((w & 0x7F7F7F7Fu) + (DT == QUICK_F16 ? 0x73737373u : 0x03030303u)) & w & 0x80808080u;
+}
+
+// Eight sums of a column to its row of out.
+template <int DT>
+__device__ __forceinline__ u4_t rounded8(const float (&v)[8], float f)
+{
+    return u4_t{to16x2<DT>(v[0] * f, v[1] * f), to16x2<DT>(v[2] * f, v[3] * f), to16x2<DT>(v[4] * f, v[5] * f),
+                to16x2<DT>(v[6] * f, v[7] * f)};
+}
+
+// Operands of two tiles of 16 channels from the same byte of eight tokens: w
+// holds four tokens of one 16 (a) and of the next (b), eight channels (W == 4)
+// or four of each; the byte's two channels go to the two operands.
+template <int DT, int W, int Y>
+__device__ __forceinline__ void value_words(const uint32_t (&a)[W], const uint32_t (&b)[W], const float (&sa)[4],
+                                            const float (&sb)[4], u4_t& lo, u4_t& hi)
+{
+    uint32_t p[8];
+    if constexpr (W == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            p[e] = code_pair<DT, Y>(a[e], sa[e]);
+            p[4 + e] = code_pair<DT, Y>(b[e], sb[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            p[2 * e] = code_pair<DT, Y>(a[e], sa[2 * e]);
+            p[2 * e + 1] = code_pair<DT, Y + 2>(a[e], sa[2 * e + 1]);
+            p[4 + 2 * e] = code_pair<DT, Y>(b[e], sb[2 * e]);
+            p[5 + 2 * e] = code_pair<DT, Y + 2>(b[e], sb[2 * e + 1]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        lo[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x05040100u);
+        hi[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x07060302u);
+    }
+}
+
+// Launches of the tiled kernel: its tiles' columns, workgroups, least share, and
+// what an item costs beside its pages.
+constexpr int kTiledColumns = 128, kTiledWorkers = 512, kTiledShare = 8, kTiledStart = 4;
+void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, hipStream_t hs);
+
+}  // namespace quick

@@ -3,10 +3,11 @@
 //
 // An item is a tile of columns (a column is a query and one of the query heads
 // that share a cache head) of a sequence for one cache head, and costs the
-// pages that some column of it sees.  Items lie in the order of sequence, tile
-// and head; a worker takes an equal run of the pages of all, so that lengths
-// may differ as they like and nothing of them is known to the host.  Items
-// that cross from one worker to the next are joined afterwards.
+// pages that some column of it sees and, before those, the time it takes to
+// begin one, in pages.  Items lie in the order of sequence, tile and head; a
+// worker takes an equal run of the cost of all, so that lengths may differ as
+// they like and nothing of them is known to the host.  Items that cross from
+// one worker to the next are joined afterwards.
 #pragma once
 #if defined(__HIPCC__)
 #include <hip/hip_runtime.h>
@@ -25,6 +26,7 @@ struct AttnShape {
     const int32_t* lengths;
     const int32_t* offsets;   // or null: one query a sequence
     int32_t T, heads, group, seqs, width, most, window, causal;
+    int32_t start;            // what an item costs beside its pages
 };
 
 // The columns of a sequence.
@@ -51,7 +53,7 @@ __device__ __host__ __forceinline__ Seq seq_of(const AttnShape& a, int b)
 
 struct Tile {
     int p0, p1;             // pages that some column sees (p1 <= p0: none)
-    int cost;               // of the item: those pages, one at least
+    int cost;               // of the item
     int columns;            // of the sequence
     int first, base, length;
     int all_lo, all_hi;     // tokens that every column sees
@@ -86,7 +88,7 @@ __device__ __host__ __forceinline__ Tile tile_of(const AttnShape& a, const Seq& 
     }
     t.p0 = begin / kPage;
     t.p1 = (int)(((int64_t)end + kPage - 1) / kPage);
-    t.cost = t.p1 - t.p0 > 1 ? t.p1 - t.p0 : 1;
+    t.cost = (t.p1 > t.p0 ? t.p1 - t.p0 : 0) + a.start;
     return t;
 }
 
@@ -100,8 +102,8 @@ __device__ __forceinline__ Tile tile_of(const AttnShape& a, int b, int j)
 
 // Where a worker stands.
 struct Walk {
-    int b, j, h, page;      // page of the item, from its first
-    int64_t left;           // pages to go
+    int b, j, h, at;        // at: how far into the item's cost
+    int64_t left;           // cost to go
     int64_t share;          // of every worker but the last
 };
 
@@ -111,7 +113,7 @@ struct PlanSpace {
     int at[4];
 };
 
-// The run of a worker, by 256 threads.  A thread adds up the pages of some
+// The run of a worker, by 256 threads.  A thread adds up the cost of some
 // sequences or, with fewer sequences than threads, of some tiles of one.
 template <int BC>
 __device__ __forceinline__ Walk find_share(const AttnShape& a, int workers, int worker, int least, PlanSpace& space)
@@ -171,18 +173,27 @@ __device__ __forceinline__ Walk find_share(const AttnShape& a, int workers, int 
     k.b = __builtin_amdgcn_readfirstlane(space.at[0]);
     k.j = __builtin_amdgcn_readfirstlane(space.at[1]);
     k.h = __builtin_amdgcn_readfirstlane(space.at[2]);
-    k.page = __builtin_amdgcn_readfirstlane(space.at[3]);
+    k.at = __builtin_amdgcn_readfirstlane(space.at[3]);
     return k;
 }
 
-// On by `take` pages of tile t.
+// The pages of tile t in a part of its cost.
+__device__ __host__ __forceinline__ void pages_of(const AttnShape& a, const Tile& t, int at, int take, int& p0, int& p1)
+{
+    const int lo = at - a.start, hi = at + take - a.start;
+    p0 = t.p0 + (lo > 0 ? lo : 0);
+    p1 = t.p0 + (hi > 0 ? hi : 0);
+    if (p1 > t.p1) p1 = t.p1;
+}
+
+// On by `take` of tile t's cost.
 template <int BC>
 __device__ __forceinline__ void advance(const AttnShape& a, Walk& k, const Tile& t, int take)
 {
     k.left -= take;
-    k.page += take;
-    if (k.page < t.cost) return;
-    k.page = 0;
+    k.at += take;
+    if (k.at < t.cost) return;
+    k.at = 0;
     if (++k.h < a.heads) return;
     k.h = 0;
     if ((int64_t)(++k.j) * BC < t.columns) return;

@@ -1,0 +1,357 @@
+// Attention over the paged 4-bit cache: many queries of a sequence.
+#include "quick_attention_parts.h"
+
+namespace quick {
+namespace {
+
+template <int DT>
+__device__ __forceinline__ f16_t mfma32(u4_t a, u4_t b, f16_t c)
+{
+    if constexpr (DT == QUICK_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(bits_as<h8_t>(a), bits_as<h8_t>(b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bits_as<b8_t>(a), bits_as<b8_t>(b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float swapped_halves(float v, int lane)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(bits_as<uint32_t>(v), bits_as<uint32_t>(v), false, false);
+    return bits_as<float>(lane < 32 ? r[1] : r[0]);
+}
+
+// What a thread holds of a page on its way to LDS.  Wave w has tokens 16 w ..
+// 16 w + 15: of the keys lane (c, g) the words of token c as in the stream
+// kernel; of the values lane (c, x, y) those of token groups x and x + 2, of
+// which it converts half y of each word.
+template <int D>
+struct Staged {
+    static constexpr int KW = D / 32, HALVES = D > 128 ? 2 : 1, VW = D < 128 ? 2 : 4;
+    uint32_t k[KW], ks[HALVES];
+    uint32_t v[HALVES][2][VW], vs[HALVES][2];
+};
+
+template <int D>
+__device__ __forceinline__ void stage(Staged<D>& s, const uint8_t* page, int wave, int lane)
+{
+    typedef Kv4<D> L;
+    typedef Staged<D> S;
+    const int c = lane & 15, g = lane >> 4, x = g & 1;
+    const uint8_t* k = page + L::kKeys + (wave * 16 + c) * (D / 2);
+#pragma unroll
+    for (int h = 0; h < S::HALVES; h++) {
+        if constexpr (D == 64) {
+            const u2_t a = *(const u2_t*)(k + g * 8);
+            s.k[0] = a[0];
+            s.k[1] = a[1];
+        } else {
+            const u4_t a = *(const u4_t*)(k + h * 64 + g * 16);
+#pragma unroll
+            for (int j = 0; j < 4; j++) s.k[h * 4 + j] = a[j];
+        }
+        s.ks[h] = *(const uint32_t*)(page + L::kKeyScales + ((D == 64 ? g >> 1 : g) + 4 * h) * 64 + c * 4);
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int group = x + 2 * i;
+            const uint8_t* v = page + L::kValues + h * 4096 + ((wave * 4 + group) * 16 + c) * (4 * S::VW);
+            if constexpr (D == 64) {
+                const u2_t a = *(const u2_t*)v;
+                s.v[h][i][0] = a[0];
+                s.v[h][i][1] = a[1];
+            } else {
+                const u4_t a = *(const u4_t*)v;
+#pragma unroll
+                for (int j = 0; j < 4; j++) s.v[h][i][j] = a[j];
+            }
+            s.vs[h][i] = *(const uint32_t*)(page + L::kValueScales + ((D == 64 ? c >> 3 : c >> 2) + 4 * h) * 64 + group * 16 + wave * 4);
+        }
+    }
+}
+
+// A page in LDS, as operands of the 32 x 32 x 16 instruction, 1 KiB each:
+// keys [32 tokens][16 channels], values [16 tokens][32 channels]; lane 32 h + r
+// holds its row r's eight of half h.  Row r of value tile i is channel
+// 128 (i / 4) + (r % 16) w + 2 (i % 4) + r / 16, w = min(D, 128) / 16; its
+// eight tokens are 16 s + 4 h + (0 .. 3) and 8 further on, which are those whose
+// scores the lane's column has.
+template <int D>
+struct Tiles {
+    u4_t k[2][D / 16][64];
+    u4_t v[4][D / 32][64];
+    uint32_t bad[4];       // whether a wave's values have blocks that the type cannot hold
+};
+
+template <int DT, int D>
+__device__ __forceinline__ void unstage(Staged<D>& s, Tiles<D>& to, int wave, int lane)
+{
+    typedef Staged<D> S;
+    const int c = lane & 15, g = lane >> 4, x = g & 1, y = g >> 1;
+    const int row = wave % 2 * 16 + c;
+#pragma unroll
+    for (int h = 0; h < S::HALVES; h++) {
+        const float scale = bits_as<float>((s.ks[h] >> (8 * wave) & 255u) << 23);
+#pragma unroll
+        for (int j = 0; j < S::KW / S::HALVES; j++) {
+            const int step = D == 64 ? g : 8 * h + 2 * g + j / 2, half = j % 2;
+            to.k[wave / 2][step][half * 32 + row] = code_words<DT>(s.k[h * 4 + j], scale);
+        }
+    }
+    uint32_t mark = 0;
+#pragma unroll
+    for (int h = 0; h < S::HALVES; h++)
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const uint32_t b = beyond<DT>(s.vs[h][i]);
+            mark |= b;
+            s.vs[h][i] &= ~((b >> 7) * 0xFFu);
+        }
+    const uint64_t any = __ballot(mark != 0);
+    if (lane == 0) to.bad[wave] = any != 0;
+#pragma unroll
+    for (int h = 0; h < S::HALVES; h++) {
+        float sa[4], sb[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            sa[e] = scale_of(s.vs[h][0], e);
+            sb[e] = scale_of(s.vs[h][1], e);
+        }
+        uint32_t a[S::VW], b[S::VW];
+#pragma unroll
+        for (int j = 0; j < S::VW; j++) {
+            // half y of each token's bytes to the front
+            a[j] = s.v[h][0][j] >> (D == 64 ? 8 * y : 16 * y);
+            b[j] = s.v[h][1][j] >> (D == 64 ? 8 * y : 16 * y);
+        }
+        u4_t lo, hi;
+        auto put = [&](int tile) {
+            to.v[wave][tile][x * 32 + c] = lo;
+            to.v[wave][tile][x * 32 + 16 + c] = hi;
+        };
+        value_words<DT, S::VW, 0>(a, b, sa, sb, lo, hi);
+        if constexpr (D == 64) put(y);
+        else {
+            put(4 * h + 2 * y);
+            value_words<DT, S::VW, 1>(a, b, sa, sb, lo, hi);
+            put(4 * h + 2 * y + 1);
+        }
+    }
+}
+
+// Blocks of values that the type cannot hold make NaN of the columns that see
+// them (they are zero in the tiles).  Seldom run.
+template <int DT, int D>
+__device__ void spoil(f16_t (&o)[D / 32], const uint8_t* page, int lo, int hi, int lane)
+{
+    typedef Kv4<D> L;
+    for (int block = 0; block < D / 32; block++) {
+        bool any = false;
+        for (int t = 0; t < kPage; t++) {
+            const uint32_t s = page[L::value_scale(t, block)];
+            any |= beyond<DT>(s) != 0 && t >= lo && t < hi;
+        }
+        if (!any) continue;
+        // a lane's rows 8 b + 4 h + i of tile j are of block 2 (b % 2) + h of their 128 channels (D == 64: b % 2)
+#pragma unroll
+        for (int j = 0; j < D / 32; j++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int b = i / 4 % 2, mine = D == 64 ? b : 4 * (j / 4) + 2 * b + (lane >> 5);
+                if (mine == block) o[j][i] = NAN;
+            }
+    }
+}
+
+// Many queries of a sequence: 128 columns (a column being a query and one of
+// the heads that share keys and values), 32 a wave.  The workgroup converts a
+// page to 16-bit operands in LDS, the next one while it multiplies; a wave has
+// its queries, its sums of values and the scores in registers.  Scores are
+// transposed, keys . queries^T, so that a lane's weights of a column are its
+// operand of values^T . weights as they stand.
+template <int DT, int D>
+__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tiled_kernel(AttnArgs a)
+{
+    typedef Kv4<D> L;
+    constexpr int BC = kTiledColumns, KS = D / 16, VT = D / 32, T = (D < 128 ? D : 128) / 16;
+    __shared__ Tiles<D> tiles[2];
+    __shared__ PlanSpace space;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5;
+    const int worker = blockIdx.x;
+    Walk walk = find_share<BC>(a.s, a.workers, worker, kTiledShare, space);
+    int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
+        const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
+        const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
+        int p0, p1;
+        pages_of(a.s, t, walk.at, take, p0, p1);
+        const int cc = walk.j * BC + wave * 32 + (lane & 31), i = cc / a.s.group;
+        const bool live = cc < t.columns, work = walk.j * BC + wave * 32 < t.columns;
+        const int pos = t.base + i;
+        const int hi = !live ? INT32_MAX : a.s.causal ? min(pos + 1, t.length) : t.length;
+        const int lo = a.s.window && live ? max(0, pos + 1 - a.s.window) : 0;
+        const int64_t head = (int64_t)walk.h * a.s.group + cc - i * a.s.group;
+        u4_t q[KS];
+        {
+            const uint8_t* from = a.q + 2 * ((int64_t)(t.first + i) * a.q_token + head * a.q_head);
+#pragma unroll
+            for (int s = 0; s < KS; s++) {
+                q[s] = u4_t{0, 0, 0, 0};
+                if (live) q[s] = *(const u4_t*)(from + (2 * s + half) * 16) ^ a.q_sign;
+            }
+        }
+        float m = kNothing, l = 0;
+        f16_t o[VT];
+#pragma unroll
+        for (int j = 0; j < VT; j++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) o[j][r] = 0;
+        const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
+        const int count = max(0, p1 - p0);
+        int32_t ids = 0;
+        Staged<D> next;
+        const uint8_t* next_page = a.cache;
+        bool next_ok = false;
+        auto fetch = [&](int n) {
+            if ((n & 63) == 0) ids = table[min(p0 + n + lane, p1 - 1)];
+            const int x = __builtin_amdgcn_readlane(ids, n & 63);
+            next_ok = x >= 0 && x < a.pages;
+            next_page = a.cache + ((int64_t)(next_ok ? x : 0) * a.s.heads + walk.h) * L::kBytes;
+            stage<D>(next, next_page, wave, lane);
+        };
+        const uint8_t* page = a.cache;
+        bool ok = false;
+        if (count) {
+            fetch(0);
+            unstage<DT, D>(next, tiles[0], wave, lane);
+            ok = next_ok;
+            page = next_page;
+            if (count > 1) fetch(1);
+            __syncthreads();
+        }
+        for (int n = 0; n < count; n++) {
+            const Tiles<D>& w = tiles[n & 1];
+            if (ok && work) {
+                const int token0 = (p0 + n) * kPage;
+                f16_t s[2];
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++) s[x][r] = 0;
+#pragma unroll
+                    for (int k = 0; k < KS; k++) s[x] = mfma32<DT>(w.k[x][k][lane], q[k], s[x]);
+                }
+                if (token0 + kPage > t.all_hi || token0 < t.all_lo) {
+#pragma unroll
+                    for (int x = 0; x < 2; x++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++) {
+                            const int token = token0 + 32 * x + r / 4 * 8 + 4 * half + r % 4;
+                            s[x][r] = token >= lo && token < hi ? s[x][r] : -INFINITY;
+                        }
+                }
+                float top = s[0][0];
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) top = fmaxf(top, s[x][r]);
+                top *= a.scale;
+                if (__ballot(top > m + kRoom)) {
+                    top = fmaxf(top, swapped_halves(top, lane));
+                    const float to = top > m + kRoom ? top - kLift : m;
+                    const float f = __builtin_amdgcn_exp2f(m - to);
+                    m = to;
+                    l *= f;
+#pragma unroll
+                    for (int j = 0; j < VT; j++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++) o[j][r] *= f;
+                }
+                u4_t p[4];
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 2) {
+                        const float u = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -m));
+                        const float v = __builtin_amdgcn_exp2f(fmaf(s[x][r + 1], a.scale, -m));
+                        l += u + v;
+                        p[2 * x + r / 8][r % 8 / 2] = to16x2<DT>(u, v);
+                    }
+                const u4_t bad = *(const u4_t*)w.bad;
+                if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) spoil<DT, D>(o, page, lo - token0, hi - token0, lane);
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+#pragma unroll
+                    for (int j = 0; j < VT; j++) o[j] = mfma32<DT>(w.v[k][j][lane], p[k], o[j]);
+            }
+            if (n + 1 < count) {
+                unstage<DT, D>(next, tiles[(n + 1) & 1], wave, lane);
+                ok = next_ok;
+                page = next_page;
+                if (n + 2 < count) fetch(n + 2);
+            }
+            __syncthreads();
+        }
+        const bool whole = walk.at == 0 && take == t.cost;
+        const int64_t slot = 2 * worker + (first ? 0 : 1);
+        if (walk.at == 0 && !whole) {
+            const int rest = t.cost - take;
+            join[0] = 1 + (int)((rest + walk.share - 1) / walk.share);
+            join[1] = walk.b;
+            join[2] = walk.j;
+            join[3] = walk.h;
+            join[4] = (int)slot;
+        }
+        if (live) {
+            l += swapped_halves(l, lane);
+            const int64_t row = (int64_t)(t.first + i) * (a.s.heads * a.s.group) + head;
+            const float f = !whole ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
+            float* part = a.part + (slot * BC + wave * 32 + (lane & 31)) * D;
+#pragma unroll
+            for (int h = 0; h < (D > 128 ? 2 : 1); h++)
+#pragma unroll
+                for (int b = 0; b < 2; b++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        const int channel = h * 128 + (8 * b + 4 * half + r) * T;
+                        float v[T];
+#pragma unroll
+                        for (int j = 0; j < T; j++) v[j] = o[h * 4 + j / 2][(b + 2 * (j % 2)) * 4 + r];
+                        if (whole) {
+                            uint8_t* to = a.out + 2 * (row * D + channel);
+                            if constexpr (T == 8) *(u4_t*)to = rounded8<DT>(v, f);
+                            else *(u2_t*)to = u2_t{to16x2<DT>(v[0] * f, v[1] * f), to16x2<DT>(v[2] * f, v[3] * f)};
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < T; j += 4) *(f4_t*)(part + channel + j) = f4_t{v[j], v[j + 1], v[j + 2], v[j + 3]};
+                        }
+                    }
+            if (half == 0) {
+                if (!whole) {
+                    a.part_ml[(slot * BC + wave * 32 + lane) * 2] = m;
+                    a.part_ml[(slot * BC + wave * 32 + lane) * 2 + 1] = l;
+                } else if (a.lse) a.lse[row] = l == 0 ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+            }
+        }
+        advance<BC>(a.s, walk, t, take);
+    }
+    if (threadIdx.x < 8) {
+        int v = join[0];
+#pragma unroll
+        for (int x = 1; x < 8; x++) v = threadIdx.x == x ? join[x] : v;
+        a.joins[worker * 8 + threadIdx.x] = v;
+    }
+}
+
+template <int DT>
+void launch(const AttnArgs& a, int64_t D, hipStream_t hs)
+{
+    if (D == 64) attn_tiled_kernel<DT, 64><<<a.workers, 256, 0, hs>>>(a);
+    else if (D == 128) attn_tiled_kernel<DT, 128><<<a.workers, 256, 0, hs>>>(a);
+    else attn_tiled_kernel<DT, 256><<<a.workers, 256, 0, hs>>>(a);
+}
+
+}  // namespace
+
+void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, hipStream_t hs)
+{
+    if (dtype == QUICK_F16) launch<QUICK_F16>(a, D, hs);
+    else launch<QUICK_BF16>(a, D, hs);
+}
+
+}  // namespace quick
