@@ -155,6 +155,7 @@ __device__ __forceinline__ void attend(PageWords<D>& w, const u4_t (&q)[NC][D / 
 #pragma unroll
     for (int n = 0; n < NC; n++) {
         if (masked) {
+            seldom();
             const int lo = seen[n].lo - token0, hi = seen[n].hi - token0;
 #pragma unroll
             for (int i = 0; i < 4; i++)
@@ -200,9 +201,9 @@ __device__ __forceinline__ void attend(PageWords<D>& w, const u4_t (&q)[NC][D / 
         u4_t pw[NC];
 #pragma unroll
         for (int n = 0; n < NC; n++)
-            pw[n] = u4_t{to16x2<DT>(p[n][2 * r][0], p[n][2 * r][1]), to16x2<DT>(p[n][2 * r][2], p[n][2 * r][3]),
-                         to16x2<DT>(p[n][2 * r + 1][0], p[n][2 * r + 1][1]),
-                         to16x2<DT>(p[n][2 * r + 1][2], p[n][2 * r + 1][3])};
+            pw[n] = u4_t{pair16<DT>(p[n][2 * r][0], p[n][2 * r][1]), pair16<DT>(p[n][2 * r][2], p[n][2 * r][3]),
+                         pair16<DT>(p[n][2 * r + 1][0], p[n][2 * r + 1][1]),
+                         pair16<DT>(p[n][2 * r + 1][2], p[n][2 * r + 1][3])};
 #pragma unroll
         for (int h = 0; h < W::HALVES; h++) {
             float sa[4], sb[4];
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
     __shared__ PlanSpace space;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int worker = blockIdx.x;
-    Walk walk = find_share<BC>(a.s, a.workers, worker, kStreamShare, space);
+    Walk walk = find_share<BC, 256>(a.s, a.workers, worker, kStreamShare, space);
     int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
         const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 int columns_of(const quick_attention_t& a)
 {
     const int64_t n = a.most * (a.q_heads / a.heads);
-    return n <= 16 ? 16 : n <= 32 ? 32 : kTiledColumns;
+    return n <= 16 ? 16 : n <= 32 ? 32 : n <= 128 || a.D > 128 ? 128 : 256;
 }
 
 int workers_of(const quick_attention_t& a)
@@ -423,8 +424,8 @@ int workers_of(const quick_attention_t& a)
     const int64_t group = a.q_heads / a.heads, bc = columns_of(a);
     const int64_t rows = std::min(a.T, a.seqs * std::min(a.most, a.T));
     const int64_t items = (std::min(a.seqs, a.T) + rows * group / bc + 1) * a.heads;
-    const int64_t least = bc == kTiledColumns ? kTiledShare : kStreamShare;
-    const int64_t most = bc == kTiledColumns ? kTiledWorkers : kStreamWorkers;
+    const int64_t least = bc > 32 ? kTiledShare : kStreamShare;
+    const int64_t most = bc == 256 ? kTiledWorkers8 : bc == 128 ? kTiledWorkers4 : kStreamWorkers;
     const int64_t shares = std::max<int64_t>(1, (a.table_width + least - 1) / least);
     return (int)(items > most / shares ? most : items * shares);
 }
@@ -439,8 +440,10 @@ void launch_attention(const AttnArgs& a, int columns, hipStream_t hs)
         attn_stream_kernel<DT, D, 2><<<a.workers, 256, 0, hs>>>(a);
         attn_join_kernel<DT, D, 32><<<a.workers, 256, 0, hs>>>(a);
     } else {
-        launch_tiled_attention(a, DT, D, hs);
-        attn_join_kernel<DT, D, kTiledColumns><<<dim3(a.workers, kTiledColumns * D / 2048), 256, 0, hs>>>(a);
+        launch_tiled_attention(a, DT, D, columns, hs);
+        const dim3 grid(a.workers, columns * D / 2048);
+        if (columns == 128) attn_join_kernel<DT, D, 128><<<grid, 256, 0, hs>>>(a);
+        else attn_join_kernel<DT, D, 256><<<grid, 256, 0, hs>>>(a);
     }
 }
 template <int DT>
@@ -501,7 +504,7 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
     a.s.most = (int32_t)std::min<int64_t>(p->most, p->T);
     a.s.window = (int32_t)std::min<int64_t>(p->window, INT32_MAX);
     a.s.causal = p->causal != 0;
-    a.s.start = columns == kTiledColumns ? kTiledStart : kStreamStart;
+    a.s.start = columns > 32 ? kTiledStart : kStreamStart;
     a.q = (const uint8_t*)q;
     a.cache = (const uint8_t*)cache;
     a.table = table;

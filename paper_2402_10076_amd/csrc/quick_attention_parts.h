@@ -48,6 +48,17 @@ __device__ __forceinline__ u4_t code_words(uint32_t w, float scale)
     return u4_t{code_pair<DT, 0>(w, scale), code_pair<DT, 1>(w, scale), code_pair<DT, 2>(w, scale),
                 code_pair<DT, 3>(w, scale)};
 }
+// Two values rounded to nearest even, as a pair.
+template <int DT>
+__device__ __forceinline__ uint32_t pair16(float a, float b)
+{
+    typedef float f2_t __attribute__((ext_vector_type(2)));
+    if constexpr (DT == QUICK_F16) return bits_as<uint32_t>(__builtin_convertvector((f2_t{a, b}), h2_t));
+    else return bits_as<uint32_t>(__builtin_convertvector((f2_t{a, b}), b2_t));
+}
+// Keeps a seldom taken branch a branch: the compiler would rather work both
+// sides out and select.
+__device__ __forceinline__ void seldom() { asm volatile("" ::); }
 // The scale that byte i of a word of scales stands for.
 __device__ __forceinline__ float scale_of(uint32_t w, int i)
 {
@@ -71,8 +82,8 @@ __device__ __forceinline__ uint32_t beyond(uint32_t w)
 template <int DT>
 __device__ __forceinline__ u4_t rounded8(const float (&v)[8], float f)
 {
-    return u4_t{to16x2<DT>(v[0] * f, v[1] * f), to16x2<DT>(v[2] * f, v[3] * f), to16x2<DT>(v[4] * f, v[5] * f),
-                to16x2<DT>(v[6] * f, v[7] * f)};
+    return u4_t{pair16<DT>(v[0] * f, v[1] * f), pair16<DT>(v[2] * f, v[3] * f), pair16<DT>(v[4] * f, v[5] * f),
+                pair16<DT>(v[6] * f, v[7] * f)};
 }
 
 // Operands of two tiles of 16 channels from the same byte of eight tokens: w
@@ -105,9 +116,9 @@ __device__ __forceinline__ void value_words(const uint32_t (&a)[W], const uint32
     }
 }
 
-// Launches of the tiled kernel: its tiles' columns, workgroups, least share, and
-// what an item costs beside its pages.
-constexpr int kTiledColumns = 128, kTiledWorkers = 512, kTiledShare = 8, kTiledStart = 4;
-void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, hipStream_t hs);
+// The tiled kernel: workgroups of four waves (128 columns) and of eight (256),
+// least share, and what an item costs beside its pages.
+constexpr int kTiledWorkers4 = 512, kTiledWorkers8 = 256, kTiledShare = 8, kTiledStart = 4;
+void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, int columns, hipStream_t hs);
 
 }  // namespace quick

@@ -109,20 +109,20 @@ struct Walk {
 
 // LDS of find_share.
 struct PlanSpace {
-    int64_t wave[4];
+    int64_t wave[8];
     int at[4];
 };
 
-// The run of a worker, by 256 threads.  A thread adds up the cost of some
+// The run of a worker, by all its N threads.  A thread adds up the cost of some
 // sequences or, with fewer sequences than threads, of some tiles of one.
-template <int BC>
+template <int BC, int N>
 __device__ __forceinline__ Walk find_share(const AttnShape& a, int workers, int worker, int least, PlanSpace& space)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int slices = a.seqs >= 256 ? 1 : 256 / a.seqs;            // threads of a sequence
-    const int per = a.seqs >= 256 ? (a.seqs + 255) / 256 : 1;       // sequences of a thread
-    const int b0 = a.seqs >= 256 ? tid * per : tid / slices;
-    const int slice = a.seqs >= 256 ? 0 : tid % slices;
+    const int slices = a.seqs >= N ? 1 : N / a.seqs;            // threads of a sequence
+    const int per = a.seqs >= N ? (a.seqs + N - 1) / N : 1;     // sequences of a thread
+    const int b0 = a.seqs >= N ? tid * per : tid / slices;
+    const int slice = a.seqs >= N ? 0 : tid % slices;
     int64_t sum = 0;
     for (int b = b0; b < min(b0 + per, a.seqs); b++) {
         const Seq s = seq_of(a, b);
@@ -139,7 +139,7 @@ __device__ __forceinline__ Walk find_share(const AttnShape& a, int workers, int 
     __syncthreads();
     int64_t all = 0, before = upto - sum;
 #pragma unroll
-    for (int w = 0; w < 4; w++) {
+    for (int w = 0; w < N / 64; w++) {
         if (w < wave) before += space.wave[w];
         all += space.wave[w];
     }

@@ -17,50 +17,51 @@ __device__ __forceinline__ float swapped_halves(float v, int lane)
     return bits_as<float>(lane < 32 ? r[1] : r[0]);
 }
 
-// What a thread holds of a page on its way to LDS.  Wave w has tokens 16 w ..
-// 16 w + 15: of the keys lane (c, g) the words of token c as in the stream
-// kernel; of the values lane (c, x, y) those of token groups x and x + 2, of
-// which it converts half y of each word.
-template <int D>
+// What a thread holds of a page on its way to LDS.  NW / 4 waves have tokens 16
+// w .. 16 w + 15: of the keys lane (c, g) the words of token c as in the stream
+// kernel, or half of them; of the values lane (c, x, y) those of token groups x
+// and x + 2, of which it converts half y of each word, or half of that.
+template <int D, int NW>
 struct Staged {
-    static constexpr int KW = D / 32, HALVES = D > 128 ? 2 : 1, VW = D < 128 ? 2 : 4;
-    uint32_t k[KW], ks[HALVES];
+    static constexpr int SHARE = NW / 4, HALVES = D > 128 ? 2 : 1, VW = D < 128 ? 2 : 4;
+    static constexpr int KW = D / 32 / HALVES / SHARE;     // words of keys of each half
+    uint32_t k[HALVES][KW], ks[HALVES];
     uint32_t v[HALVES][2][VW], vs[HALVES][2];
 };
 
-template <int D>
-__device__ __forceinline__ void stage(Staged<D>& s, const uint8_t* page, int wave, int lane)
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&to)[N], const uint8_t* from)
+{
+    if constexpr (N == 1) to[0] = *(const uint32_t*)from;
+    else if constexpr (N == 2) {
+        const u2_t a = *(const u2_t*)from;
+        to[0] = a[0];
+        to[1] = a[1];
+    } else {
+        const u4_t a = *(const u4_t*)from;
+#pragma unroll
+        for (int j = 0; j < 4; j++) to[j] = a[j];
+    }
+}
+
+template <int D, int NW>
+__device__ __forceinline__ void stage(Staged<D, NW>& s, const uint8_t* page, int wave, int lane)
 {
     typedef Kv4<D> L;
-    typedef Staged<D> S;
-    const int c = lane & 15, g = lane >> 4, x = g & 1;
-    const uint8_t* k = page + L::kKeys + (wave * 16 + c) * (D / 2);
+    typedef Staged<D, NW> S;
+    const int c = lane & 15, g = lane >> 4, x = g & 1, w = wave / S::SHARE, part = wave % S::SHARE;
+    const uint32_t key = L::kKeys + (w * 16 + c) * (D / 2) + g * (D == 64 ? 8 : 16) + part * 4 * S::KW;
+    const uint32_t key_scale = L::kKeyScales + (D == 64 ? g >> 1 : g) * 64 + c * 4;
+    const uint32_t value = L::kValues + ((w * 4 + x) * 16 + c) * (4 * S::VW);
+    const uint32_t value_scale = L::kValueScales + (D == 64 ? c >> 3 : c >> 2) * 64 + x * 16 + w * 4;
 #pragma unroll
     for (int h = 0; h < S::HALVES; h++) {
-        if constexpr (D == 64) {
-            const u2_t a = *(const u2_t*)(k + g * 8);
-            s.k[0] = a[0];
-            s.k[1] = a[1];
-        } else {
-            const u4_t a = *(const u4_t*)(k + h * 64 + g * 16);
-#pragma unroll
-            for (int j = 0; j < 4; j++) s.k[h * 4 + j] = a[j];
-        }
-        s.ks[h] = *(const uint32_t*)(page + L::kKeyScales + ((D == 64 ? g >> 1 : g) + 4 * h) * 64 + c * 4);
+        load_words(s.k[h], page + key + h * 64);
+        s.ks[h] = *(const uint32_t*)(page + key_scale + h * 256);
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            const int group = x + 2 * i;
-            const uint8_t* v = page + L::kValues + h * 4096 + ((wave * 4 + group) * 16 + c) * (4 * S::VW);
-            if constexpr (D == 64) {
-                const u2_t a = *(const u2_t*)v;
-                s.v[h][i][0] = a[0];
-                s.v[h][i][1] = a[1];
-            } else {
-                const u4_t a = *(const u4_t*)v;
-#pragma unroll
-                for (int j = 0; j < 4; j++) s.v[h][i][j] = a[j];
-            }
-            s.vs[h][i] = *(const uint32_t*)(page + L::kValueScales + ((D == 64 ? c >> 3 : c >> 2) + 4 * h) * 64 + group * 16 + wave * 4);
+            load_words(s.v[h][i], page + value + h * 4096 + i * (128 * S::VW));
+            s.vs[h][i] = *(const uint32_t*)(page + value_scale + h * 256 + i * 32);
         }
     }
 }
@@ -78,34 +79,27 @@ struct Tiles {
     uint32_t bad[4];       // whether a wave's values have blocks that the type cannot hold
 };
 
-template <int DT, int D>
-__device__ __forceinline__ void unstage(Staged<D>& s, Tiles<D>& to, int wave, int lane)
+template <int DT, int D, int NW>
+__device__ __forceinline__ void unstage(Staged<D, NW>& s, Tiles<D>& to, int wave, int lane)
 {
-    typedef Staged<D> S;
-    const int c = lane & 15, g = lane >> 4, x = g & 1, y = g >> 1;
-    const int row = wave % 2 * 16 + c;
-#pragma unroll
-    for (int h = 0; h < S::HALVES; h++) {
-        const float scale = bits_as<float>((s.ks[h] >> (8 * wave) & 255u) << 23);
-#pragma unroll
-        for (int j = 0; j < S::KW / S::HALVES; j++) {
-            const int step = D == 64 ? g : 8 * h + 2 * g + j / 2, half = j % 2;
-            to.k[wave / 2][step][half * 32 + row] = code_words<DT>(s.k[h * 4 + j], scale);
-        }
-    }
+    typedef Staged<D, NW> S;
+    const int c = lane & 15, g = lane >> 4, x = g & 1, y = g >> 1, w = wave / S::SHARE, part = wave % S::SHARE;
     uint32_t mark = 0;
 #pragma unroll
-    for (int h = 0; h < S::HALVES; h++)
+    for (int h = 0; h < S::HALVES; h++) {
+        const float scale = bits_as<float>((s.ks[h] >> (8 * w) & 255u) << 23);
+#pragma unroll
+        for (int j = 0; j < S::KW; j++) {
+            // word n of a lane: channels 8 n .. of its 32 (D == 64: 16)
+            const int n = part * S::KW + j, step = D == 64 ? g : 8 * h + 2 * g + n / 2;
+            to.k[w / 2][step][n % 2 * 32 + w % 2 * 16 + c] = code_words<DT>(s.k[h][j], scale);
+        }
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             const uint32_t b = beyond<DT>(s.vs[h][i]);
             mark |= b;
             s.vs[h][i] &= ~((b >> 7) * 0xFFu);
         }
-    const uint64_t any = __ballot(mark != 0);
-    if (lane == 0) to.bad[wave] = any != 0;
-#pragma unroll
-    for (int h = 0; h < S::HALVES; h++) {
         float sa[4], sb[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
@@ -115,23 +109,30 @@ __device__ __forceinline__ void unstage(Staged<D>& s, Tiles<D>& to, int wave, in
         uint32_t a[S::VW], b[S::VW];
 #pragma unroll
         for (int j = 0; j < S::VW; j++) {
-            // half y of each token's bytes to the front
-            a[j] = s.v[h][0][j] >> (D == 64 ? 8 * y : 16 * y);
-            b[j] = s.v[h][1][j] >> (D == 64 ? 8 * y : 16 * y);
+            // this lane's bytes of each token to the front
+            const int by = D == 64 ? 8 * y : 16 * y + 8 * part;
+            a[j] = s.v[h][0][j] >> by;
+            b[j] = s.v[h][1][j] >> by;
         }
         u4_t lo, hi;
         auto put = [&](int tile) {
-            to.v[wave][tile][x * 32 + c] = lo;
-            to.v[wave][tile][x * 32 + 16 + c] = hi;
+            to.v[w][tile][x * 32 + c] = lo;
+            to.v[w][tile][x * 32 + 16 + c] = hi;
         };
         value_words<DT, S::VW, 0>(a, b, sa, sb, lo, hi);
-        if constexpr (D == 64) put(y);
-        else {
-            put(4 * h + 2 * y);
-            value_words<DT, S::VW, 1>(a, b, sa, sb, lo, hi);
-            put(4 * h + 2 * y + 1);
+        if constexpr (D == 64) {
+            // (with eight waves both of a pair write the same)
+            put(y);
+        } else {
+            put(4 * h + 2 * y + part);
+            if constexpr (S::SHARE == 1) {
+                value_words<DT, S::VW, 1>(a, b, sa, sb, lo, hi);
+                put(4 * h + 2 * y + 1);
+            }
         }
     }
+    const uint64_t any = __ballot(mark != 0);
+    to.bad[w] = any != 0;     // (every lane the same)
 }
 
 // Blocks of values that the type cannot hold make NaN of the columns that see
@@ -158,22 +159,39 @@ __device__ void spoil(f16_t (&o)[D / 32], const uint8_t* page, int lo, int hi, i
     }
 }
 
-// Many queries of a sequence: 128 columns (a column being a query and one of
+// The order of the end of a half page: the matrix instructions of the values
+// with the vector instructions of the next page's conversion.
+template <int N>
+__device__ __forceinline__ void interleave()
+{
+    constexpr int kMfma = 8, kRead = 0x100, kWrite = 0x200, kValu = 2;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        if (i < N - 4) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kValu, 56 / N, 0);
+        if (i % 2) __builtin_amdgcn_sched_group_barrier(kWrite, 1, 0);
+    }
+}
+
+// Many queries of a sequence: 32 NW columns (a column being a query and one of
 // the heads that share keys and values), 32 a wave.  The workgroup converts a
 // page to 16-bit operands in LDS, the next one while it multiplies; a wave has
 // its queries, its sums of values and the scores in registers.  Scores are
 // transposed, keys . queries^T, so that a lane's weights of a column are its
-// operand of values^T . weights as they stand.
-template <int DT, int D>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tiled_kernel(AttnArgs a)
+// operand of values^T . weights as they stand.  Half a page at a time, and the
+// scores of the next half beside the weights of this one, so that the matrix
+// instructions of the one run under the vector instructions of the other.
+template <int DT, int D, int NW, int NB>
+__global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(AttnArgs a)
 {
     typedef Kv4<D> L;
-    constexpr int BC = kTiledColumns, KS = D / 16, VT = D / 32, T = (D < 128 ? D : 128) / 16;
-    __shared__ Tiles<D> tiles[2];
+    constexpr int BC = 32 * NW, KS = D / 16, VT = D / 32, T = (D < 128 ? D : 128) / 16;
+    __shared__ Tiles<D> tiles[NB];
     __shared__ PlanSpace space;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5;
     const int worker = blockIdx.x;
-    Walk walk = find_share<BC>(a.s, a.workers, worker, kTiledShare, space);
+    Walk walk = find_share<BC, 64 * NW>(a.s, a.workers, worker, kTiledShare, space);
     int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
         const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
@@ -203,90 +221,137 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tiled_kernel(AttnAr
             for (int r = 0; r < 16; r++) o[j][r] = 0;
         const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
         const int count = max(0, p1 - p0);
-        int32_t ids = 0;
-        Staged<D> next;
+        Staged<D, NW> next;
         const uint8_t* next_page = a.cache;
         bool next_ok = false;
+        int id = 0;
+        // page n to registers (the id of the one after it, too); behind the last one that again
         auto fetch = [&](int n) {
-            if ((n & 63) == 0) ids = table[min(p0 + n + lane, p1 - 1)];
-            const int x = __builtin_amdgcn_readlane(ids, n & 63);
+            const int x = (int)uniform((uint32_t)id);
+            id = table[min(p0 + n + 1, p1 - 1)];
             next_ok = x >= 0 && x < a.pages;
             next_page = a.cache + ((int64_t)(next_ok ? x : 0) * a.s.heads + walk.h) * L::kBytes;
-            stage<D>(next, next_page, wave, lane);
+            stage<D, NW>(next, next_page, wave, lane);
         };
-        const uint8_t* page = a.cache;
+        // scores of half x of a page
+        auto scores = [&](const Tiles<D>& w, int x, f16_t& s) {
+#pragma unroll
+            for (int r = 0; r < 16; r++) s[r] = 0;
+#pragma unroll
+            for (int k = 0; k < KS; k++) s = mfma32<DT>(w.k[x][k][lane], q[k], s);
+        };
+        // hides what a column does not see of those, and sets its reference
+        auto refer = [&](f16_t& s, int token0, bool ok) {
+            if (token0 + 32 > t.all_hi || token0 < t.all_lo || !ok) {
+                seldom();
+                const int to = ok ? hi : INT32_MIN;
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    const int token = token0 + r / 4 * 8 + 4 * half + r % 4;
+                    s[r] = token >= lo && token < to ? s[r] : -INFINITY;
+                }
+            }
+            float top = s[0];
+#pragma unroll
+            for (int r = 0; r < 16; r++) top = fmaxf(top, s[r]);
+            top *= a.scale;
+            if (__ballot(top > m + kRoom)) {
+                seldom();
+                top = fmaxf(top, swapped_halves(top, lane));
+                const float to = top > m + kRoom ? top - kLift : m;
+                const float f = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= f;
+#pragma unroll
+                for (int j = 0; j < VT; j++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) o[j][r] *= f;
+            }
+        };
+        // Half x of page w: s's weights and the values they weigh; beside them the scores s1 of half x1 of page w1.
+        // Each step of those has a matrix instruction, a load of an operand four steps ahead and a share of the
+        // weights, and the compiler is kept from gathering them.
+        auto half_page = [&](const Tiles<D>& w, int x, const f16_t& s, const Tiles<D>& w1, int x1, f16_t& s1) {
+            constexpr int AHEAD = 4, PV = 2 * VT;
+            u4_t p[2], f[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++) f[k] = w1.k[x1][k][lane];
+#pragma unroll
+            for (int r = 0; r < 16; r++) s1[r] = 0;
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                __builtin_amdgcn_sched_barrier(0);
+                s1 = mfma32<DT>(f[k % AHEAD], q[k], s1);
+                if (k + AHEAD < KS) f[k % AHEAD] = w1.k[x1][k + AHEAD][lane];
+                else f[k % AHEAD] = w.v[2 * x + (k + AHEAD - KS) / VT][(k + AHEAD - KS) % VT][lane];
+#pragma unroll
+                for (int r = 16 * k / KS / 2 * 2; r < 16 * (k + 1) / KS / 2 * 2; r += 2) {
+                    const float u = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -m));
+                    const float v = __builtin_amdgcn_exp2f(fmaf(s[r + 1], a.scale, -m));
+                    l += u + v;
+                    p[r / 8][r % 8 / 2] = pair16<DT>(u, v);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < PV; k++) {
+                o[k % VT] = mfma32<DT>(f[k % AHEAD], p[k / VT], o[k % VT]);
+                if (k + AHEAD < PV) f[k % AHEAD] = w.v[2 * x + (k + AHEAD) / VT][(k + AHEAD) % VT][lane];
+            }
+        };
+        const uint8_t *page = a.cache, *page1 = a.cache;
         bool ok = false;
+        f16_t s;
+        int at = 0;
         if (count) {
+            id = table[p0];
             fetch(0);
-            unstage<DT, D>(next, tiles[0], wave, lane);
+            unstage<DT, D, NW>(next, tiles[0], wave, lane);
             ok = next_ok;
             page = next_page;
-            if (count > 1) fetch(1);
+            fetch(1);
             __syncthreads();
+            if (work) scores(tiles[0], 0, s);
         }
         for (int n = 0; n < count; n++) {
-            const Tiles<D>& w = tiles[n & 1];
-            if (ok && work) {
-                const int token0 = (p0 + n) * kPage;
-                f16_t s[2];
-#pragma unroll
-                for (int x = 0; x < 2; x++) {
-#pragma unroll
-                    for (int r = 0; r < 16; r++) s[x][r] = 0;
-#pragma unroll
-                    for (int k = 0; k < KS; k++) s[x] = mfma32<DT>(w.k[x][k][lane], q[k], s[x]);
+            const Tiles<D>& w = tiles[at];
+            const int to = at + 1 == NB ? 0 : at + 1;
+            const int token0 = (p0 + n) * kPage;
+            f16_t s1;
+            bool ok1 = false;
+            // (behind the last page that one again, which nothing reads)
+            auto on = [&] {
+                unstage<DT, D, NW>(next, tiles[to], wave, lane);
+                ok1 = next_ok;
+                page1 = next_page;
+                fetch(n + 2);
+            };
+            if (work) {
+                refer(s, token0, ok);
+                half_page(w, 0, s, w, 1, s1);
+                if constexpr (NB > 2) {
+                    on();
+                    interleave<2 * VT>();
                 }
-                if (token0 + kPage > t.all_hi || token0 < t.all_lo) {
-#pragma unroll
-                    for (int x = 0; x < 2; x++)
-#pragma unroll
-                        for (int r = 0; r < 16; r++) {
-                            const int token = token0 + 32 * x + r / 4 * 8 + 4 * half + r % 4;
-                            s[x][r] = token >= lo && token < hi ? s[x][r] : -INFINITY;
-                        }
-                }
-                float top = s[0][0];
-#pragma unroll
-                for (int x = 0; x < 2; x++)
-#pragma unroll
-                    for (int r = 0; r < 16; r++) top = fmaxf(top, s[x][r]);
-                top *= a.scale;
-                if (__ballot(top > m + kRoom)) {
-                    top = fmaxf(top, swapped_halves(top, lane));
-                    const float to = top > m + kRoom ? top - kLift : m;
-                    const float f = __builtin_amdgcn_exp2f(m - to);
-                    m = to;
-                    l *= f;
-#pragma unroll
-                    for (int j = 0; j < VT; j++)
-#pragma unroll
-                        for (int r = 0; r < 16; r++) o[j][r] *= f;
-                }
-                u4_t p[4];
-#pragma unroll
-                for (int x = 0; x < 2; x++)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 2) {
-                        const float u = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -m));
-                        const float v = __builtin_amdgcn_exp2f(fmaf(s[x][r + 1], a.scale, -m));
-                        l += u + v;
-                        p[2 * x + r / 8][r % 8 / 2] = to16x2<DT>(u, v);
-                    }
-                const u4_t bad = *(const u4_t*)w.bad;
-                if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) spoil<DT, D>(o, page, lo - token0, hi - token0, lane);
-#pragma unroll
-                for (int k = 0; k < 4; k++)
-#pragma unroll
-                    for (int j = 0; j < VT; j++) o[j] = mfma32<DT>(w.v[k][j][lane], p[k], o[j]);
-            }
-            if (n + 1 < count) {
-                unstage<DT, D>(next, tiles[(n + 1) & 1], wave, lane);
-                ok = next_ok;
-                page = next_page;
-                if (n + 2 < count) fetch(n + 2);
+            } else if (NB > 2) on();
+            if constexpr (NB == 2) {
+                // the tile that is overwritten now has been read
+                __syncthreads();
+                on();
             }
             __syncthreads();
+            if (work) {
+                refer(s1, token0 + 32, ok);
+                half_page(w, 1, s1, tiles[to], 0, s);
+                const u4_t bad = *(const u4_t*)w.bad;
+                if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) spoil<DT, D>(o, page, lo - token0, (ok ? hi : 0) - token0, lane);
+            }
+            ok = ok1;
+            page = page1;
+            at = to;
         }
+        // the next item's first page goes where the last one's lies
+        __syncthreads();
         const bool whole = walk.at == 0 && take == t.cost;
         const int64_t slot = 2 * worker + (first ? 0 : 1);
         if (walk.at == 0 && !whole) {
@@ -315,7 +380,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tiled_kernel(AttnAr
                         if (whole) {
                             uint8_t* to = a.out + 2 * (row * D + channel);
                             if constexpr (T == 8) *(u4_t*)to = rounded8<DT>(v, f);
-                            else *(u2_t*)to = u2_t{to16x2<DT>(v[0] * f, v[1] * f), to16x2<DT>(v[2] * f, v[3] * f)};
+                            else *(u2_t*)to = u2_t{pair16<DT>(v[0] * f, v[1] * f), pair16<DT>(v[2] * f, v[3] * f)};
                         } else {
 #pragma unroll
                             for (int j = 0; j < T; j += 4) *(f4_t*)(part + channel + j) = f4_t{v[j], v[j + 1], v[j + 2], v[j + 3]};
@@ -338,20 +403,28 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tiled_kernel(AttnAr
     }
 }
 
-template <int DT>
-void launch(const AttnArgs& a, int64_t D, hipStream_t hs)
+template <int DT, int D>
+void launch(const AttnArgs& a, int columns, hipStream_t hs)
 {
-    if (D == 64) attn_tiled_kernel<DT, 64><<<a.workers, 256, 0, hs>>>(a);
-    else if (D == 128) attn_tiled_kernel<DT, 128><<<a.workers, 256, 0, hs>>>(a);
-    else attn_tiled_kernel<DT, 256><<<a.workers, 256, 0, hs>>>(a);
+    if constexpr (D <= 128) {
+        if (columns == 256) return attn_tiled_kernel<DT, D, 8, 3><<<a.workers, 512, 0, hs>>>(a);
+    }
+    attn_tiled_kernel<DT, D, 4, 2><<<a.workers, 256, 0, hs>>>(a);
+}
+template <int DT>
+void launch(const AttnArgs& a, int64_t D, int columns, hipStream_t hs)
+{
+    if (D == 64) launch<DT, 64>(a, columns, hs);
+    else if (D == 128) launch<DT, 128>(a, columns, hs);
+    else launch<DT, 256>(a, columns, hs);
 }
 
 }  // namespace
 
-void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, hipStream_t hs)
+void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, int columns, hipStream_t hs)
 {
-    if (dtype == QUICK_F16) launch<QUICK_F16>(a, D, hs);
-    else launch<QUICK_BF16>(a, D, hs);
+    if (dtype == QUICK_F16) launch<QUICK_F16>(a, D, columns, hs);
+    else launch<QUICK_BF16>(a, D, columns, hs);
 }
 
 }  // namespace quick
