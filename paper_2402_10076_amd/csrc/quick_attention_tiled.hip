@@ -79,61 +79,66 @@ struct Tiles {
     uint32_t bad[4];       // whether a wave's values have blocks that the type cannot hold
 };
 
+// In four steps, so that a caller can put them between other instructions.
 template <int DT, int D, int NW>
-__device__ __forceinline__ void unstage(Staged<D, NW>& s, Tiles<D>& to, int wave, int lane)
-{
+struct Unstage {
     typedef Staged<D, NW> S;
-    const int c = lane & 15, g = lane >> 4, x = g & 1, y = g >> 1, w = wave / S::SHARE, part = wave % S::SHARE;
-    uint32_t mark = 0;
-#pragma unroll
-    for (int h = 0; h < S::HALVES; h++) {
-        const float scale = bits_as<float>((s.ks[h] >> (8 * w) & 255u) << 23);
-#pragma unroll
-        for (int j = 0; j < S::KW; j++) {
-            // word n of a lane: channels 8 n .. of its 32 (D == 64: 16)
-            const int n = part * S::KW + j, step = D == 64 ? g : 8 * h + 2 * g + n / 2;
-            to.k[w / 2][step][n % 2 * 32 + w % 2 * 16 + c] = code_words<DT>(s.k[h][j], scale);
+    float sa[S::HALVES][4], sb[S::HALVES][4];
+    uint32_t a[S::HALVES][S::VW], b[S::HALVES][S::VW], mark;
+
+    template <int STEP>
+    __device__ __forceinline__ void step(Staged<D, NW>& s, Tiles<D>& to, int wave, int lane)
+    {
+        const int c = lane & 15, g = lane >> 4, x = g & 1, y = g >> 1, w = wave / S::SHARE, part = wave % S::SHARE;
+        if constexpr (STEP == 0) mark = 0;
+        if constexpr (STEP == 3) {
+            const uint64_t any = __ballot(mark != 0);
+            to.bad[w] = any != 0;     // (every lane the same)
         }
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const uint32_t b = beyond<DT>(s.vs[h][i]);
-            mark |= b;
-            s.vs[h][i] &= ~((b >> 7) * 0xFFu);
-        }
-        float sa[4], sb[4];
+        for (int h = 0; h < S::HALVES; h++) {
+            if constexpr (STEP == 0) {
+                const float scale = bits_as<float>((s.ks[h] >> (8 * w) & 255u) << 23);
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            sa[e] = scale_of(s.vs[h][0], e);
-            sb[e] = scale_of(s.vs[h][1], e);
-        }
-        uint32_t a[S::VW], b[S::VW];
+                for (int j = 0; j < S::KW; j++) {
+                    // word n of a lane: channels 8 n .. of its 32 (D == 64: 16)
+                    const int n = part * S::KW + j, step = D == 64 ? g : 8 * h + 2 * g + n / 2;
+                    to.k[w / 2][step][n % 2 * 32 + w % 2 * 16 + c] = code_words<DT>(s.k[h][j], scale);
+                }
+            }
+            if constexpr (STEP == 1) {
 #pragma unroll
-        for (int j = 0; j < S::VW; j++) {
-            // this lane's bytes of each token to the front
-            const int by = D == 64 ? 8 * y : 16 * y + 8 * part;
-            a[j] = s.v[h][0][j] >> by;
-            b[j] = s.v[h][1][j] >> by;
-        }
-        u4_t lo, hi;
-        auto put = [&](int tile) {
-            to.v[w][tile][x * 32 + c] = lo;
-            to.v[w][tile][x * 32 + 16 + c] = hi;
-        };
-        value_words<DT, S::VW, 0>(a, b, sa, sb, lo, hi);
-        if constexpr (D == 64) {
-            // (with eight waves both of a pair write the same)
-            put(y);
-        } else {
-            put(4 * h + 2 * y + part);
-            if constexpr (S::SHARE == 1) {
-                value_words<DT, S::VW, 1>(a, b, sa, sb, lo, hi);
-                put(4 * h + 2 * y + 1);
+                for (int i = 0; i < 2; i++) {
+                    const uint32_t b = beyond<DT>(s.vs[h][i]);
+                    mark |= b;
+                    s.vs[h][i] &= ~((b >> 7) * 0xFFu);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    sa[h][e] = scale_of(s.vs[h][0], e);
+                    sb[h][e] = scale_of(s.vs[h][1], e);
+                }
+#pragma unroll
+                for (int j = 0; j < S::VW; j++) {
+                    // this lane's bytes of each token to the front
+                    const int by = D == 64 ? 8 * y : 16 * y + 8 * part;
+                    a[h][j] = s.v[h][0][j] >> by;
+                    b[h][j] = s.v[h][1][j] >> by;
+                }
+            }
+            if constexpr (STEP >= 2) {
+                u4_t lo, hi;
+                // (D == 64: with eight waves both of a pair write the same)
+                const int tile = D == 64 ? y : 4 * h + (S::SHARE == 1 ? 2 * y + STEP - 2 : 2 * y + part);
+                if constexpr (STEP == 2 || (D > 64 && S::SHARE == 1)) {
+                    value_words<DT, S::VW, STEP - 2>(a[h], b[h], sa[h], sb[h], lo, hi);
+                    to.v[w][tile][x * 32 + c] = lo;
+                    to.v[w][tile][x * 32 + 16 + c] = hi;
+                }
             }
         }
     }
-    const uint64_t any = __ballot(mark != 0);
-    to.bad[w] = any != 0;     // (every lane the same)
-}
+};
 
 // Blocks of values that the type cannot hold make NaN of the columns that see
 // them (they are zero in the tiles).  Seldom run.
@@ -156,21 +161,6 @@ __device__ void spoil(f16_t (&o)[D / 32], const uint8_t* page, int lo, int hi, i
                 const int b = i / 4 % 2, mine = D == 64 ? b : 4 * (j / 4) + 2 * b + (lane >> 5);
                 if (mine == block) o[j][i] = NAN;
             }
-    }
-}
-
-// The order of the end of a half page: the matrix instructions of the values
-// with the vector instructions of the next page's conversion.
-template <int N>
-__device__ __forceinline__ void interleave()
-{
-    constexpr int kMfma = 8, kRead = 0x100, kWrite = 0x200, kValu = 2;
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-        if (i < N - 4) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kValu, 56 / N, 0);
-        if (i % 2) __builtin_amdgcn_sched_group_barrier(kWrite, 1, 0);
     }
 }
 
@@ -271,11 +261,14 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
         // Half x of page w: s's weights and the values they weigh; beside them the scores s1 of half x1 of page w1.
         // Each step of those has a matrix instruction, a load of an operand four steps ahead and a share of the
         // weights, and the compiler is kept from gathering them.
-        auto half_page = [&](const Tiles<D>& w, int x, const f16_t& s, const Tiles<D>& w1, int x1, f16_t& s1) {
-            constexpr int AHEAD = 4, PV = 2 * VT;
-            u4_t p[2], f[AHEAD];
+        constexpr int AHEAD = 4, PV = 2 * VT;
+        u4_t f[AHEAD];
+        auto first_operands = [&](const Tiles<D>& w1, int x1) {
 #pragma unroll
             for (int k = 0; k < AHEAD; k++) f[k] = w1.k[x1][k][lane];
+        };
+        auto half_page = [&](const Tiles<D>& w, int x, const f16_t& s, const Tiles<D>& w1, int x1, f16_t& s1, auto beside) {
+            u4_t p[2];
 #pragma unroll
             for (int r = 0; r < 16; r++) s1[r] = 0;
 #pragma unroll
@@ -297,6 +290,8 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             for (int k = 0; k < PV; k++) {
                 o[k % VT] = mfma32<DT>(f[k % AHEAD], p[k / VT], o[k % VT]);
                 if (k + AHEAD < PV) f[k % AHEAD] = w.v[2 * x + (k + AHEAD) / VT][(k + AHEAD) % VT][lane];
+                beside(k);
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
         const uint8_t *page = a.cache, *page1 = a.cache;
@@ -306,7 +301,11 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
         if (count) {
             id = table[p0];
             fetch(0);
-            unstage<DT, D, NW>(next, tiles[0], wave, lane);
+            Unstage<DT, D, NW> un;
+            un.template step<0>(next, tiles[0], wave, lane);
+            un.template step<1>(next, tiles[0], wave, lane);
+            un.template step<2>(next, tiles[0], wave, lane);
+            un.template step<3>(next, tiles[0], wave, lane);
             ok = next_ok;
             page = next_page;
             fetch(1);
@@ -319,30 +318,41 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             const int token0 = (p0 + n) * kPage;
             f16_t s1;
             bool ok1 = false;
+            Unstage<DT, D, NW> un;
             // (behind the last page that one again, which nothing reads)
-            auto on = [&] {
-                unstage<DT, D, NW>(next, tiles[to], wave, lane);
-                ok1 = next_ok;
-                page1 = next_page;
-                fetch(n + 2);
+            auto on = [&](int k) {
+                if (k == 0) un.template step<0>(next, tiles[to], wave, lane);
+                if (k == PV / 4) un.template step<1>(next, tiles[to], wave, lane);
+                if (k == PV / 2) un.template step<2>(next, tiles[to], wave, lane);
+                if (k == 3 * PV / 4) {
+                    un.template step<3>(next, tiles[to], wave, lane);
+                    ok1 = next_ok;
+                    page1 = next_page;
+                    fetch(n + 2);
+                }
+            };
+            auto all_on = [&] {
+                on(0);
+                on(PV / 4);
+                on(PV / 2);
+                on(3 * PV / 4);
             };
             if (work) {
+                first_operands(w, 1);
                 refer(s, token0, ok);
-                half_page(w, 0, s, w, 1, s1);
-                if constexpr (NB > 2) {
-                    on();
-                    interleave<2 * VT>();
-                }
-            } else if (NB > 2) on();
+                if constexpr (NB > 2) half_page(w, 0, s, w, 1, s1, on);
+                else half_page(w, 0, s, w, 1, s1, [](int) {});
+            } else if (NB > 2) all_on();
             if constexpr (NB == 2) {
                 // the tile that is overwritten now has been read
                 __syncthreads();
-                on();
+                all_on();
             }
             __syncthreads();
             if (work) {
+                first_operands(tiles[to], 0);
                 refer(s1, token0 + 32, ok);
-                half_page(w, 1, s1, tiles[to], 0, s);
+                half_page(w, 1, s1, tiles[to], 0, s, [](int) {});
                 const u4_t bad = *(const u4_t*)w.bad;
                 if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) spoil<DT, D>(o, page, lo - token0, (ok ? hi : 0) - token0, lane);
             }
