@@ -8,8 +8,11 @@ namespace {
 
 using namespace quick;
 
-// Workgroups of the stream kernel: three for each compute unit.
-constexpr int kStreamWorkers = 768;
+// Workgroups of the stream kernel that a compute unit holds at once, by the
+// registers that D channels and NC times 16 columns take; the grid is that for
+// all units.
+constexpr int stream_resident(int64_t D, int NC) { return (D == 64 ? 5 : D == 128 ? 4 : 3) - NC; }
+constexpr int kUnits = 256;
 // What a workgroup takes at least, and what an item costs beside its pages.
 constexpr int kStreamShare = 8, kStreamStart = 4;
 
@@ -27,43 +30,58 @@ __device__ __forceinline__ float over_groups(float v, F f)
 // of tokens c of each 16, its quarter of the channels; of the values of tokens
 // 4 g .. 4 g + 3 of each 16, channels c * w .. c * w + w - 1 of each 128.
 template <int D>
-struct PageWords {
-    static constexpr int KW = D / 32, HALVES = D > 128 ? 2 : 1, VW = D < 128 ? 2 : 4;
-    uint32_t k[4][KW], ks[HALVES];
-    uint32_t v[HALVES][4][VW], vs[HALVES][4];
+struct KeyWords {
+    static constexpr int KW = D / 32, HALVES = D > 128 ? 2 : 1;
+    uint32_t k[4][KW], s[HALVES];
+};
+template <int D>
+struct ValueWords {
+    static constexpr int HALVES = D > 128 ? 2 : 1, VW = D < 128 ? 2 : 4;
+    uint32_t v[HALVES][4][VW], s[HALVES][4];
 };
 
 template <int D>
-__device__ __forceinline__ void load_page(PageWords<D>& w, const uint8_t* page, int lane)
+__device__ __forceinline__ void load_keys(KeyWords<D>& w, const uint8_t* page, int lane)
 {
     typedef Kv4<D> L;
-    typedef PageWords<D> W;
-    const int c = lane & 15, g = lane >> 4;
+    const uint32_t c = lane & 15, g = lane >> 4;
+    const uint32_t key = L::kKeys + c * (D / 2) + g * (D == 64 ? 8 : 16);
+    const uint32_t scale = L::kKeyScales + (D == 64 ? g >> 1 : g) * 64 + c * 4;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const uint8_t* k = page + L::kKeys + (i * 16 + c) * (D / 2);
-        if constexpr (D == 64) {
-            const u2_t a = *(const u2_t*)(k + g * 8);
-            w.k[i][0] = a[0];
-            w.k[i][1] = a[1];
-        } else {
+    for (int h = 0; h < KeyWords<D>::HALVES; h++) {
+        w.s[h] = *(const uint32_t*)(page + scale + h * 256);
 #pragma unroll
-            for (int h = 0; h < W::HALVES; h++) {
-                const u4_t a = *(const u4_t*)(k + h * 64 + g * 16);
+        for (int i = 0; i < 4; i++) {
+            const uint8_t* k = page + key + i * (8 * D) + h * 64;
+            if constexpr (D == 64) {
+                const u2_t a = *(const u2_t*)k;
+                w.k[i][0] = a[0];
+                w.k[i][1] = a[1];
+            } else {
+                const u4_t a = *(const u4_t*)k;
 #pragma unroll
                 for (int j = 0; j < 4; j++) w.k[i][h * 4 + j] = a[j];
             }
         }
     }
+}
+
+template <int D>
+__device__ __forceinline__ void load_values(ValueWords<D>& w, const uint8_t* page, int lane)
+{
+    typedef Kv4<D> L;
+    constexpr int VW = ValueWords<D>::VW;
+    const uint32_t c = lane & 15, g = lane >> 4;
+    const uint32_t value = L::kValues + (g * 16 + c) * (4 * VW);
+    const uint32_t scale = L::kValueScales + (D == 64 ? c >> 3 : c >> 2) * 64 + g * 16;
 #pragma unroll
-    for (int h = 0; h < W::HALVES; h++) {
-        w.ks[h] = *(const uint32_t*)(page + L::kKeyScales + ((D == 64 ? g >> 1 : g) + 4 * h) * 64 + c * 4);
-        const u4_t s = *(const u4_t*)(page + L::kValueScales + ((D == 64 ? c >> 3 : c >> 2) + 4 * h) * 64 + g * 16);
+    for (int h = 0; h < ValueWords<D>::HALVES; h++) {
+        const u4_t s = *(const u4_t*)(page + scale + h * 256);
 #pragma unroll
-        for (int i = 0; i < 4; i++) w.vs[h][i] = s[i];
+        for (int i = 0; i < 4; i++) w.s[h][i] = s[i];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const uint8_t* v = page + L::kValues + h * 4096 + ((i * 4 + g) * 16 + c) * (4 * W::VW);
+            const uint8_t* v = page + value + h * 4096 + i * (256 * VW);
             if constexpr (D == 64) {
                 const u2_t a = *(const u2_t*)v;
                 w.v[h][i][0] = a[0];
@@ -95,9 +113,9 @@ struct Seen {
 // see them, and nothing of the others: they are taken out of the product (their
 // scales become 2^-127) and the sums of those columns set.  Seldom run.
 template <int DT, int D>
-__device__ void take_out(PageWords<D>& w, Column<D>& col, Seen seen, int token0, int lane, bool clear)
+__device__ void take_out(ValueWords<D>& w, Column<D>& col, Seen seen, int token0, int lane, bool clear)
 {
-    typedef PageWords<D> W;
+    typedef ValueWords<D> W;
     constexpr int TILES = (D < 128 ? D : 128) / 16;
     const int g = lane >> 4, block = D == 64 ? g >> 1 : g;
 #pragma unroll
@@ -105,7 +123,7 @@ __device__ void take_out(PageWords<D>& w, Column<D>& col, Seen seen, int token0,
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const uint32_t mark = beyond<DT>(w.vs[h][i]);
+            const uint32_t mark = beyond<DT>(w.s[h][i]);
             for (int e = 0; e < 4; e++) {
                 // lane 16 x + (first lane of a block) has token 16 i + 4 x + e of that block
                 const uint64_t b = __ballot(mark >> (8 * e + 7) & 1);
@@ -114,7 +132,7 @@ __device__ void take_out(PageWords<D>& w, Column<D>& col, Seen seen, int token0,
                     bad |= (b >> (16 * x + block * (D == 64 ? 8 : 4)) & 1) && token >= seen.lo && token < seen.hi;
                 }
             }
-            if (clear) w.vs[h][i] &= ~((mark >> 7) * 0xFFu);
+            if (clear) w.s[h][i] &= ~((mark >> 7) * 0xFFu);
         }
         if (bad) {
 #pragma unroll
@@ -123,54 +141,50 @@ __device__ void take_out(PageWords<D>& w, Column<D>& col, Seen seen, int token0,
     }
 }
 
-// One page into NC columns of a wave.
+// Scores of a page's keys with the NC columns of a lane (16 tokens each 16).
 template <int DT, int D, int NC>
-__device__ __forceinline__ void attend(PageWords<D>& w, const u4_t (&q)[NC][D / 32], Column<D> (&col)[NC],
-                                       const Seen (&seen)[NC], int token0, bool masked, float scale, int lane)
+__device__ __forceinline__ void score(const KeyWords<D>& w, const u4_t (&q)[NC][D / 32], f4_t (&s)[NC][4])
 {
-    typedef PageWords<D> W;
-    constexpr int KW = W::KW, TILES = (D < 128 ? D : 128) / 16;
-    const int g = lane >> 4;
-    float p[NC][4][4];
-    {
-        f4_t s[NC][4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+    for (int i = 0; i < 4; i++) {
 #pragma unroll
-            for (int n = 0; n < NC; n++) s[n][i] = f4_t{0, 0, 0, 0};
+        for (int n = 0; n < NC; n++) s[n][i] = f4_t{0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < KW; j++) {
-                const u4_t k = code_words<DT>(w.k[i][j], scale_of(w.ks[j / 4], i));
+        for (int j = 0; j < D / 32; j++) {
+            const u4_t k = code_words<DT>(w.k[i][j], scale_of(w.s[j / 4], i));
 #pragma unroll
-                for (int n = 0; n < NC; n++) s[n][i] = mfma16<DT>(k, q[n][j], s[n][i]);
-            }
+            for (int n = 0; n < NC; n++) s[n][i] = mfma16<DT>(k, q[n][j], s[n][i]);
         }
-#pragma unroll
-        for (int n = 0; n < NC; n++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) p[n][i][e] = s[n][i][e] * scale;
     }
+}
+
+// The weights of those, as operands p[n][r] of 32 tokens each.
+template <int DT, int D, int NC>
+__device__ __forceinline__ void weigh(f4_t (&s)[NC][4], Column<D> (&col)[NC], const Seen (&seen)[NC], int token0, bool masked,
+                                      bool ok, float scale, int lane, u4_t (&p)[NC][2])
+{
+    const int g = lane >> 4;
 #pragma unroll
     for (int n = 0; n < NC; n++) {
         if (masked) {
             seldom();
-            const int lo = seen[n].lo - token0, hi = seen[n].hi - token0;
+            const int lo = seen[n].lo - token0, hi = ok ? seen[n].hi - token0 : 0;
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     const int t = 16 * i + 4 * g + e;
-                    p[n][i][e] = t >= lo && t < hi ? p[n][i][e] : -INFINITY;
+                    s[n][i][e] = t >= lo && t < hi ? s[n][i][e] : -INFINITY;
                 }
         }
-        float top = p[n][0][0];
+        float top = s[n][0][0];
 #pragma unroll
         for (int i = 0; i < 4; i++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) top = fmaxf(top, p[n][i][e]);
+            for (int e = 0; e < 4; e++) top = fmaxf(top, s[n][i][e]);
+        top *= scale;
         if (__ballot(top > col[n].m + kRoom)) {
+            seldom();
             top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
             const float m = top > col[n].m + kRoom ? top - kLift : col[n].m;
             const float f = __builtin_amdgcn_exp2f(col[n].m - m);
@@ -182,42 +196,37 @@ __device__ __forceinline__ void attend(PageWords<D>& w, const u4_t (&q)[NC][D / 
 #pragma unroll
         for (int i = 0; i < 4; i++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                p[n][i][e] = __builtin_amdgcn_exp2f(p[n][i][e] - col[n].m);
-                col[n].l += p[n][i][e];
+            for (int e = 0; e < 4; e += 2) {
+                const float u = __builtin_amdgcn_exp2f(fmaf(s[n][i][e], scale, -col[n].m));
+                const float v = __builtin_amdgcn_exp2f(fmaf(s[n][i][e + 1], scale, -col[n].m));
+                col[n].l += u + v;
+                p[n][i / 2][i % 2 * 2 + e / 2] = pair16<DT>(u, v);
             }
     }
-    uint32_t mark = 0;
-#pragma unroll
-    for (int h = 0; h < W::HALVES; h++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) mark |= beyond<DT>(w.vs[h][i]);
-    if (__ballot(mark != 0)) {
-#pragma unroll
-        for (int n = 0; n < NC; n++) take_out<DT, D>(w, col[n], seen[n], token0, lane, n == NC - 1);
-    }
+}
+
+// The values that those weigh.
+template <int DT, int D, int NC>
+__device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&p)[NC][2], Column<D> (&col)[NC])
+{
+    typedef ValueWords<D> W;
+    constexpr int TILES = (D < 128 ? D : 128) / 16;
 #pragma unroll
     for (int r = 0; r < 2; r++) {
-        u4_t pw[NC];
-#pragma unroll
-        for (int n = 0; n < NC; n++)
-            pw[n] = u4_t{pair16<DT>(p[n][2 * r][0], p[n][2 * r][1]), pair16<DT>(p[n][2 * r][2], p[n][2 * r][3]),
-                         pair16<DT>(p[n][2 * r + 1][0], p[n][2 * r + 1][1]),
-                         pair16<DT>(p[n][2 * r + 1][2], p[n][2 * r + 1][3])};
 #pragma unroll
         for (int h = 0; h < W::HALVES; h++) {
             float sa[4], sb[4];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                sa[e] = scale_of(w.vs[h][2 * r], e);
-                sb[e] = scale_of(w.vs[h][2 * r + 1], e);
+                sa[e] = scale_of(w.s[h][2 * r], e);
+                sb[e] = scale_of(w.s[h][2 * r + 1], e);
             }
             u4_t lo, hi;
             auto add = [&](int j) {
 #pragma unroll
                 for (int n = 0; n < NC; n++) {
-                    col[n].o[h * TILES + j] = mfma16<DT>(lo, pw[n], col[n].o[h * TILES + j]);
-                    col[n].o[h * TILES + j + 1] = mfma16<DT>(hi, pw[n], col[n].o[h * TILES + j + 1]);
+                    col[n].o[h * TILES + j] = mfma16<DT>(lo, p[n][r], col[n].o[h * TILES + j]);
+                    col[n].o[h * TILES + j + 1] = mfma16<DT>(hi, p[n][r], col[n].o[h * TILES + j + 1]);
                 }
             };
             value_words<DT, W::VW, 0>(w.v[h][2 * r], w.v[h][2 * r + 1], sa, sb, lo, hi);
@@ -241,7 +250,7 @@ __device__ __forceinline__ void attend(PageWords<D>& w, const u4_t (&q)[NC][D / 
 // values^T . weights, with no exchange between lanes and nothing in LDS; the
 // waves' sums meet in LDS once an item.
 template <int DT, int D, int NC>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kernel(AttnArgs a)
 {
     typedef Kv4<D> L;
     constexpr int BC = 16 * NC, KW = D / 32, TILES = (D < 128 ? D : 128) / 16, ROW = D + 4;
@@ -283,25 +292,44 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
         }
         const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
         int32_t ids = 0;
-        PageWords<D> cur;
-        auto fetch = [&](int n, PageWords<D>& to) {    // page n of this wave
+        auto page_of = [&](int n, bool& inside) {    // page n of this wave
             if ((n & 63) == 0) ids = table[min(p0 + wave + 4 * (n + lane), p1 - 1)];
             const int x = __builtin_amdgcn_readlane(ids, n & 63);
-            const bool inside = x >= 0 && x < a.pages;
-            load_page<D>(to, a.cache + ((int64_t)(inside ? x : 0) * a.s.heads + walk.h) * L::kBytes, lane);
-            return inside;
+            inside = x >= 0 && x < a.pages;
+            return a.cache + ((int64_t)(inside ? x : 0) * a.s.heads + walk.h) * L::kBytes;
         };
         const int count = p1 > p0 + wave ? (p1 - p0 - wave + 3) / 4 : 0;
+        KeyWords<D> keys;
+        ValueWords<D> values;
         bool ok = false;
-        if (count) ok = fetch(0, cur);
+        if (count) {
+            const uint8_t* page = page_of(0, ok);
+            load_keys<D>(keys, page, lane);
+            load_values<D>(values, page, lane);
+        }
         for (int n = 0; n < count; n++) {
-            PageWords<D> next;
-            bool next_ok = false;
-            if (n + 1 < count) next_ok = fetch(n + 1, next);
             const int token0 = (p0 + wave + 4 * n) * kPage;
-            const bool masked = token0 + kPage > t.all_hi || token0 < t.all_lo;
-            if (ok) attend<DT, D, NC>(cur, q, col, seen, token0, masked, a.scale, lane);
-            cur = next;
+            const bool masked = token0 + kPage > t.all_hi || token0 < t.all_lo || !ok;
+            f4_t s[NC][4];
+            u4_t p[NC][2];
+            score<DT, D, NC>(keys, q, s);
+            // the next page's keys and values take the place of this one's as those are done with (the last one's again)
+            bool next_ok;
+            const uint8_t* next = page_of(min(n + 1, count - 1), next_ok);
+            load_keys<D>(keys, next, lane);
+            weigh<DT, D, NC>(s, col, seen, token0, masked, ok, a.scale, lane, p);
+            uint32_t mark = 0;
+#pragma unroll
+            for (int h = 0; h < ValueWords<D>::HALVES; h++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) mark |= beyond<DT>(values.s[h][i]);
+            if (__ballot(mark != 0)) {
+                seldom();
+#pragma unroll
+                for (int x = 0; x < NC; x++) take_out<DT, D>(values, col[x], Seen{seen[x].lo, ok ? seen[x].hi : 0}, token0, lane, x == NC - 1);
+            }
+            add_values<DT, D, NC>(values, p, col);
+            load_values<D>(values, next, lane);
             ok = next_ok;
         }
         const bool whole = walk.at == 0 && take == t.cost;
@@ -323,7 +351,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
                 refs[wave][c][1] = l;
             }
 #pragma unroll
-            for (int h = 0; h < PageWords<D>::HALVES; h++)
+            for (int h = 0; h < ValueWords<D>::HALVES; h++)
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     float* to = &sums[wave][c][h * 128 + (4 * g + i) * TILES];
@@ -425,7 +453,7 @@ int workers_of(const quick_attention_t& a)
     const int64_t rows = std::min(a.T, a.seqs * std::min(a.most, a.T));
     const int64_t items = (std::min(a.seqs, a.T) + rows * group / bc + 1) * a.heads;
     const int64_t least = bc > 32 ? kTiledShare : kStreamShare;
-    const int64_t most = bc == 256 ? kTiledWorkers8 : bc == 128 ? kTiledWorkers4 : kStreamWorkers;
+    const int64_t most = bc == 256 ? kTiledWorkers8 : bc == 128 ? kTiledWorkers4 : kUnits * stream_resident(a.D, (int)bc / 16);
     const int64_t shares = std::max<int64_t>(1, (a.table_width + least - 1) / least);
     return (int)(items > most / shares ? most : items * shares);
 }

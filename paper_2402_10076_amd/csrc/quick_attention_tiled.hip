@@ -271,6 +271,7 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             u4_t p[2];
 #pragma unroll
             for (int r = 0; r < 16; r++) s1[r] = 0;
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int k = 0; k < KS; k++) {
                 __builtin_amdgcn_sched_barrier(0);
@@ -286,6 +287,7 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int k = 0; k < PV; k++) {
                 o[k % VT] = mfma32<DT>(f[k % AHEAD], p[k / VT], o[k % VT]);
