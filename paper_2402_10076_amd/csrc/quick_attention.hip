@@ -11,7 +11,7 @@ using namespace quick;
 // Workgroups of the stream kernel that a compute unit holds at once, by the
 // registers that D channels and NC times 16 columns take; the grid is that for
 // all units.
-constexpr int stream_resident(int64_t D, int NC) { return (D == 64 ? 5 : D == 128 ? 4 : 3) - NC; }
+constexpr int stream_resident(int64_t D, int NC) { return D == 64 ? 6 - 2 * NC : (D == 128 ? 4 : 3) - NC; }
 constexpr int kUnits = 256;
 // What a workgroup takes at least, and what an item costs beside its pages.
 constexpr int kStreamShare = 8, kStreamStart = 4;
@@ -113,31 +113,30 @@ struct Seen {
 // see them, and nothing of the others: they are taken out of the product (their
 // scales become 2^-127) and the sums of those columns set.  Seldom run.
 template <int DT, int D>
-__device__ void take_out(ValueWords<D>& w, Column<D>& col, Seen seen, int token0, int lane, bool clear)
+__device__ __forceinline__ void take_out(ValueWords<D>& w)
 {
-    typedef ValueWords<D> W;
+#pragma unroll
+    for (int h = 0; h < ValueWords<D>::HALVES; h++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) w.s[h][i] &= ~((beyond<DT>(w.s[h][i]) >> 7) * 0xFFu);
+}
+template <int DT, int D>
+__device__ __forceinline__ void spoil(Column<D>& col, const uint8_t* page, int lo, int hi, int lane)
+{
+    typedef Kv4<D> L;
     constexpr int TILES = (D < 128 ? D : 128) / 16;
-    const int g = lane >> 4, block = D == 64 ? g >> 1 : g;
+    const int g = lane >> 4;
 #pragma unroll
-    for (int h = 0; h < W::HALVES; h++) {
+    for (int h = 0; h < ValueWords<D>::HALVES; h++) {
         bool bad = false;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint32_t mark = beyond<DT>(w.s[h][i]);
-            for (int e = 0; e < 4; e++) {
-                // lane 16 x + (first lane of a block) has token 16 i + 4 x + e of that block
-                const uint64_t b = __ballot(mark >> (8 * e + 7) & 1);
-                for (int x = 0; x < 4; x++) {
-                    const int token = token0 + 16 * i + 4 * x + e;
-                    bad |= (b >> (16 * x + block * (D == 64 ? 8 : 4)) & 1) && token >= seen.lo && token < seen.hi;
-                }
-            }
-            if (clear) w.s[h][i] &= ~((mark >> 7) * 0xFFu);
+#pragma unroll 1
+        for (int t = 0; t < kPage; t++) {
+            const uint32_t s = page[L::value_scale(t, (D == 64 ? g >> 1 : g) + 4 * h)];
+            bad |= beyond<DT>(s) != 0 && t >= lo && t < hi;
         }
-        if (bad) {
+        const float f = bad ? NAN : 0.0f;
 #pragma unroll
-            for (int j = 0; j < TILES; j++) col.o[h * TILES + j] = f4_t{NAN, NAN, NAN, NAN};
-        }
+        for (int j = 0; j < TILES; j++) col.o[h * TILES + j] += f;
     }
 }
 
@@ -302,8 +301,9 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
         KeyWords<D> keys;
         ValueWords<D> values;
         bool ok = false;
+        const uint8_t* page = a.cache;
         if (count) {
-            const uint8_t* page = page_of(0, ok);
+            page = page_of(0, ok);
             load_keys<D>(keys, page, lane);
             load_values<D>(values, page, lane);
         }
@@ -326,10 +326,13 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
             if (__ballot(mark != 0)) {
                 seldom();
 #pragma unroll
-                for (int x = 0; x < NC; x++) take_out<DT, D>(values, col[x], Seen{seen[x].lo, ok ? seen[x].hi : 0}, token0, lane, x == NC - 1);
+                for (int x = 0; x < NC; x++)
+                    spoil<DT, D>(col[x], page, seen[x].lo - token0, ok ? seen[x].hi - token0 : 0, lane);
+                take_out<DT, D>(values);
             }
             add_values<DT, D, NC>(values, p, col);
             load_values<D>(values, next, lane);
+            page = next;
             ok = next_ok;
         }
         const bool whole = walk.at == 0 && take == t.cost;
