@@ -11,10 +11,10 @@ using namespace quick;
 // Workgroups of the stream kernel that a compute unit holds at once, by the
 // registers that D channels and NC times 16 columns take; the grid is that for
 // all units.
-constexpr int stream_resident(int64_t D, int NC) { return D == 64 ? 6 - 2 * NC : (D == 128 ? 4 : 3) - NC; }
+constexpr int stream_resident(int64_t D, int NC) { return D == 64 ? 6 - 2 * NC : D == 128 ? 2 : 3 - NC; }
 constexpr int kUnits = 256;
 // What a workgroup takes at least, and what an item costs beside its pages.
-constexpr int kStreamShare = 8, kStreamStart = 4;
+constexpr int kStreamShare = 16, kStreamStart = 12;
 
 // Exchanges over the four groups of 16 lanes that share a column.
 template <class F>
@@ -242,36 +242,42 @@ __device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&
     }
 }
 
-// A few queries of each sequence (16 NC columns, a column being a query and one
-// of the heads that share keys and values).  A wave takes every fourth page of
-// its workgroup's share: scores transposed, keys . queries^T, so that a
+// A few queries of each sequence (16 NC columns at most, a column being a query
+// and one of the heads that share keys and values).  A wave takes every WAVES'th page
+// of its workgroup's share: scores transposed, keys . queries^T, so that a
 // column's scores are in the lanes that need its weights as the operand of
 // values^T . weights, with no exchange between lanes and nothing in LDS; the
 // waves' sums meet in LDS once an item.
-template <int DT, int D, int NC>
-__global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kernel(AttnArgs a)
+template <int DT, int D, int NC, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_stream_kernel(AttnArgs a)
 {
     typedef Kv4<D> L;
     constexpr int BC = 16 * NC, KW = D / 32, TILES = (D < 128 ? D : 128) / 16, ROW = D + 4;
-    __shared__ float sums[4][16][ROW];
-    __shared__ float refs[4][16][2];
-    __shared__ PlanSpace space;
+    __shared__ float sums[WAVES][16][ROW];
+    __shared__ float refs[WAVES][16][2];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int worker = blockIdx.x;
-    Walk walk = find_share<BC, 256>(a.s, a.workers, worker, kStreamShare, space);
+    Walk walk;
+    if (a.whole) {
+        // an item each: no joining
+        walk.b = worker / a.s.heads;
+        walk.h = worker - walk.b * a.s.heads;
+        walk.j = walk.at = 0;
+        walk.left = walk.share = INT32_MAX;
+    } else walk = find_share<BC, false>(a.s, a.workers, worker, kStreamShare);
     int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
-        const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
+        const Tile t = tile_of<BC>(a.s, walk.b, 0);
         const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
+        if (left_to_next(a.s, walk, t, take)) break;
         int p0, p1;
         pages_of(a.s, t, walk.at, take, p0, p1);
-        const int col0 = walk.j * BC;
         u4_t q[NC][KW];
         Column<D> col[NC];
         Seen seen[NC];
 #pragma unroll
         for (int n = 0; n < NC; n++) {
-            const int cc = col0 + n * 16 + c, i = cc / a.s.group;
+            const int cc = n * 16 + c, i = cc * a.group_inv >> 16;
             const bool live = cc < t.columns;
             const int pos = t.base + i;
             seen[n].hi = !live ? INT32_MAX : a.s.causal ? min(pos + 1, t.length) : t.length;
@@ -292,12 +298,12 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
         const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
         int32_t ids = 0;
         auto page_of = [&](int n, bool& inside) {    // page n of this wave
-            if ((n & 63) == 0) ids = table[min(p0 + wave + 4 * (n + lane), p1 - 1)];
+            if ((n & 63) == 0) ids = table[min(p0 + wave + WAVES * (n + lane), p1 - 1)];
             const int x = __builtin_amdgcn_readlane(ids, n & 63);
             inside = x >= 0 && x < a.pages;
             return a.cache + ((int64_t)(inside ? x : 0) * a.s.heads + walk.h) * L::kBytes;
         };
-        const int count = p1 > p0 + wave ? (p1 - p0 - wave + 3) / 4 : 0;
+        const int count = p1 > p0 + wave ? (p1 - p0 - wave + WAVES - 1) / WAVES : 0;
         KeyWords<D> keys;
         ValueWords<D> values;
         bool ok = false;
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
             load_values<D>(values, page, lane);
         }
         for (int n = 0; n < count; n++) {
-            const int token0 = (p0 + wave + 4 * n) * kPage;
+            const int token0 = (p0 + wave + WAVES * n) * kPage;
             const bool masked = token0 + kPage > t.all_hi || token0 < t.all_lo || !ok;
             f4_t s[NC][4];
             u4_t p[NC][2];
@@ -338,12 +344,7 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
         const bool whole = walk.at == 0 && take == t.cost;
         const int64_t slot = 2 * worker + (first ? 0 : 1);
         if (walk.at == 0 && !whole) {
-            const int rest = t.cost - take;
-            join[0] = 1 + (int)((rest + walk.share - 1) / walk.share);    // parts
-            join[1] = walk.b;
-            join[2] = walk.j;
-            join[3] = walk.h;
-            join[4] = (int)slot;
+            set_join(join, walk, t, BC, take, (int)slot);
         }
 #pragma unroll
         for (int n = 0; n < NC; n++) {
@@ -365,22 +366,22 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
                 }
             __syncthreads();
             constexpr int PIECES = D / 8;
-            for (int at = threadIdx.x; at < 16 * PIECES; at += 256) {
-                const int x = at / PIECES, d = at % PIECES * 8, cc = col0 + n * 16 + x;
+            for (int at = threadIdx.x; at < 16 * PIECES; at += 64 * WAVES) {
+                const int x = at / PIECES, d = at % PIECES * 8, cc = n * 16 + x;
                 if (cc >= t.columns) continue;
                 float m = refs[0][x][0];
 #pragma unroll
-                for (int w = 1; w < 4; w++) m = fmaxf(m, refs[w][x][0]);
+                for (int w = 1; w < WAVES; w++) m = fmaxf(m, refs[w][x][0]);
                 float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0;
 #pragma unroll
-                for (int w = 0; w < 4; w++) {
+                for (int w = 0; w < WAVES; w++) {
                     const float f = __builtin_amdgcn_exp2f(refs[w][x][0] - m);
                     sum += refs[w][x][1] * f;
 #pragma unroll
                     for (int j = 0; j < 8; j++) v[j] += sums[w][x][d + j] * f;
                 }
                 if (whole) {
-                    const int i = cc / a.s.group;
+                    const int i = cc * a.group_inv >> 16;
                     const int64_t row = (int64_t)(t.first + i) * (a.s.heads * a.s.group) + walk.h * a.s.group + cc - i * a.s.group;
                     *(u4_t*)(a.out + 2 * (row * D + d)) = rounded8<DT>(v, sum == 0 ? 0.0f : 1.0f / sum);
                     if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
@@ -395,7 +396,8 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
                 }
             }
         }
-        advance<BC>(a.s, walk, t, take);
+        if (a.whole) return;
+        advance<BC, false>(a.s, walk, t, take);
     }
     if (threadIdx.x < 8) {
         int v = join[0];
@@ -406,40 +408,42 @@ __global__ __launch_bounds__(256, stream_resident(D, NC)) void attn_stream_kerne
 }
 
 // Joins the parts of the item that a worker left unfinished: its own, and the
-// first ones of the workers after it.  A thread has eight channels of a column.
+// first ones of the workers after it.  A thread has eight channels of a column;
+// the parts' references first, so that the loads of their sums are independent
+// of each other.
 template <int DT, int D, int BC>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
     const int worker = blockIdx.x;
-    const int parts = a.joins[worker * 8];
+    const int32_t* join = a.joins + worker * 8;
+    const int parts = join[0], slot0 = join[1], col0 = join[2], columns = join[3], first = join[4], h = join[5];
     if (parts == 0) return;
-    const int b = a.joins[worker * 8 + 1], j = a.joins[worker * 8 + 2], h = a.joins[worker * 8 + 3];
-    const int64_t slot0 = a.joins[worker * 8 + 4];
-    const Tile t = tile_of<BC>(a.s, b, j);
     constexpr int PIECES = D / 8;
-    for (int at = threadIdx.x + 256 * blockIdx.y; at < BC * PIECES; at += 256 * gridDim.y) {
-        const int x = at / PIECES, d = at % PIECES * 8, cc = j * BC + x;
-        if (cc >= t.columns) continue;
-        float m = kNothing, sum = 0, v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int i = 0; i < parts; i++) {
-            const int64_t slot = i == 0 ? slot0 : 2 * (int64_t)(worker + i);
-            const float* ml = a.part_ml + (slot * BC + x) * 2;
-            const f4_t* from = (const f4_t*)(a.part + ((slot * BC + x) * D + d));
-            const f4_t p = from[0], r = from[1];
-            const float n = fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - n), e = __builtin_amdgcn_exp2f(ml[0] - n);
-            m = n;
-            sum = sum * f + ml[1] * e;
+    const int at = threadIdx.x + 256 * blockIdx.y, x = at / PIECES, d = at % PIECES * 8, cc = col0 + x;
+    if (x >= BC || cc >= columns) return;
+    auto place = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (worker + i)) * BC + x; };
+    float m = kNothing;
+#pragma unroll 4
+    for (int i = 0; i < parts; i++) m = fmaxf(m, a.part_ml[place(i) * 2]);
+    float sum = 0, v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+    for (int i = 0; i < parts; i++) {
+        const int64_t p = place(i);
+        const float* ml = a.part_ml + p * 2;
+        const f4_t* from = (const f4_t*)(a.part + p * D + d);
+        const f4_t u = from[0], w = from[1];
+        const float f = __builtin_amdgcn_exp2f(ml[0] - m);
+        sum += ml[1] * f;
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                v[k] = v[k] * f + p[k] * e;
-                v[4 + k] = v[4 + k] * f + r[k] * e;
-            }
+        for (int k = 0; k < 4; k++) {
+            v[k] += u[k] * f;
+            v[4 + k] += w[k] * f;
         }
-        const int i = cc / a.s.group;
-        const int64_t row = (int64_t)(t.first + i) * (a.s.heads * a.s.group) + h * a.s.group + cc - i * a.s.group;
-        *(u4_t*)(a.out + 2 * (row * D + d)) = rounded8<DT>(v, sum == 0 ? 0.0f : 1.0f / sum);
-        if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
     }
+    const int i = cc / a.s.group;
+    const int64_t row = (int64_t)(first + i) * (a.s.heads * a.s.group) + h * a.s.group + cc - i * a.s.group;
+    *(u4_t*)(a.out + 2 * (row * D + d)) = rounded8<DT>(v, sum == 0 ? 0.0f : 1.0f / sum);
+    if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
 }
 
 // Columns of a workgroup's tile.
@@ -449,10 +453,15 @@ int columns_of(const quick_attention_t& a)
     return n <= 16 ? 16 : n <= 32 ? 32 : n <= 128 || a.D > 128 ? 128 : 256;
 }
 
+// Whether a workgroup takes an item each: few queries of sequences of 16 pages
+// at most, for which a second launch costs more than unequal lengths do.
+bool whole_items(const quick_attention_t& a) { return columns_of(a) <= 32 && a.table_width <= 16; }
+
 int workers_of(const quick_attention_t& a)
 {
     // no more than there can be pages of items
     const int64_t group = a.q_heads / a.heads, bc = columns_of(a);
+    if (whole_items(a)) return (int)(a.seqs * a.heads);
     const int64_t rows = std::min(a.T, a.seqs * std::min(a.most, a.T));
     const int64_t items = (std::min(a.seqs, a.T) + rows * group / bc + 1) * a.heads;
     const int64_t least = bc > 32 ? kTiledShare : kStreamShare;
@@ -461,16 +470,25 @@ int workers_of(const quick_attention_t& a)
     return (int)(items > most / shares ? most : items * shares);
 }
 
+template <int DT, int D, int NC>
+void launch_stream(const AttnArgs& a, hipStream_t hs)
+{
+    if (a.whole) {
+        // few items: more waves each (whose registers do not suffice for 32 columns of 256 channels)
+        if constexpr (D * NC < 512) {
+            if (a.workers <= 2 * kUnits) return attn_stream_kernel<DT, D, NC, 8><<<a.workers, 512, 0, hs>>>(a);
+        }
+        return attn_stream_kernel<DT, D, NC, 4><<<a.workers, 256, 0, hs>>>(a);
+    }
+    attn_stream_kernel<DT, D, NC, 4><<<a.workers, 256, 0, hs>>>(a);
+    attn_join_kernel<DT, D, 16 * NC><<<dim3(a.workers, (2 * NC * D + 255) / 256), 256, 0, hs>>>(a);
+}
 template <int DT, int D>
 void launch_attention(const AttnArgs& a, int columns, hipStream_t hs)
 {
-    if (columns == 16) {
-        attn_stream_kernel<DT, D, 1><<<a.workers, 256, 0, hs>>>(a);
-        attn_join_kernel<DT, D, 16><<<a.workers, 256, 0, hs>>>(a);
-    } else if (columns == 32) {
-        attn_stream_kernel<DT, D, 2><<<a.workers, 256, 0, hs>>>(a);
-        attn_join_kernel<DT, D, 32><<<a.workers, 256, 0, hs>>>(a);
-    } else {
+    if (columns == 16) launch_stream<DT, D, 1>(a, hs);
+    else if (columns == 32) launch_stream<DT, D, 2>(a, hs);
+    else {
         launch_tiled_attention(a, DT, D, columns, hs);
         const dim3 grid(a.workers, columns * D / 2048);
         if (columns == 128) attn_join_kernel<DT, D, 128><<<grid, 256, 0, hs>>>(a);
@@ -502,7 +520,7 @@ int check_attention(const quick_attention_t& a)
 
 extern "C" size_t quick_kv4_attention_workspace_bytes(const quick_attention_t* p)
 {
-    if (!p || check_attention(*p) || p->T == 0 || p->seqs == 0) return 0;
+    if (!p || check_attention(*p) || p->T == 0 || p->seqs == 0 || whole_items(*p)) return 0;
     const size_t w = (size_t)workers_of(*p), c = (size_t)columns_of(*p);
     return w * 32 + 2 * w * c * ((size_t)p->D + 2) * sizeof(float);
 }
@@ -520,16 +538,18 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
         !aligned(offsets, 4) || !aligned(lse, 4) || p->q_token % 8 || p->q_head % 8)
         return QUICK_ERR_ALIGNMENT;
     const size_t need = quick_kv4_attention_workspace_bytes(p);
-    if (!workspace || workspace_bytes < need) return QUICK_ERR_WORKSPACE;
+    if (need && (!workspace || workspace_bytes < need)) return QUICK_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return QUICK_ERR_ALIGNMENT;
     AttnArgs a{};
     a.workers = workers_of(*p);
+    a.whole = whole_items(*p);
     const int columns = columns_of(*p);
     a.s.lengths = lengths;
     a.s.offsets = offsets;
     a.s.T = (int32_t)p->T;
     a.s.heads = (int32_t)p->heads;
     a.s.group = (int32_t)(p->q_heads / p->heads);
+    a.group_inv = (65535 + a.s.group) / a.s.group;
     a.s.seqs = (int32_t)p->seqs;
     a.s.width = (int32_t)p->table_width;
     a.s.most = (int32_t)std::min<int64_t>(p->most, p->T);
@@ -541,9 +561,11 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
     a.table = table;
     a.out = (uint8_t*)out;
     a.lse = lse;
-    a.joins = (int32_t*)workspace;
-    a.part = (float*)((uint8_t*)workspace + (size_t)a.workers * 32);
-    a.part_ml = a.part + 2 * (size_t)a.workers * columns * p->D;
+    if (need) {
+        a.joins = (int32_t*)workspace;
+        a.part = (float*)((uint8_t*)workspace + (size_t)a.workers * 32);
+        a.part_ml = a.part + 2 * (size_t)a.workers * columns * p->D;
+    }
     a.q_token = p->q_token;
     a.q_head = p->q_head;
     a.pages = (int32_t)p->pages;

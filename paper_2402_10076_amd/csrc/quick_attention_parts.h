@@ -31,9 +31,23 @@ struct AttnArgs {
     int32_t* joins;       // [workers][8] the item that a worker leaves unfinished
     int64_t q_token, q_head;
     int32_t pages, workers;
+    int32_t group_inv;    // c / group == c * group_inv >> 16 for c < 32
+    int32_t whole;        // a worker takes an item and no more; nothing to join
     float scale;          // of the scores times log2(e), without its sign
     uint32_t q_sign;      // changes q's sign where the scale is negative
 };
+
+// What the joining kernel is told of an item that a worker leaves unfinished.
+__device__ __forceinline__ void set_join(int (&join)[8], const Walk& w, const Tile& t, int columns, int take, int slot)
+{
+    const int rest = t.cost - take;
+    join[0] = 1 + (int)((rest + w.share - 1) / w.share);    // parts
+    join[1] = slot;
+    join[2] = w.j * columns;
+    join[3] = t.columns;
+    join[4] = t.first;
+    join[5] = w.h;
+}
 
 // Two values of byte BYTE of a word of codes times the scale, as 16-bit pair.
 template <int DT, int BYTE>
@@ -118,7 +132,7 @@ __device__ __forceinline__ void value_words(const uint32_t (&a)[W], const uint32
 
 // The tiled kernel: workgroups of four waves (128 columns) and of eight (256),
 // least share, and what an item costs beside its pages.
-constexpr int kTiledWorkers4 = 512, kTiledWorkers8 = 256, kTiledShare = 8, kTiledStart = 4;
+constexpr int kTiledWorkers4 = 512, kTiledWorkers8 = 256, kTiledShare = 10, kTiledStart = 6;
 void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, int columns, hipStream_t hs);
 
 }  // namespace quick

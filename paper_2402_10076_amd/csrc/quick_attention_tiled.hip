@@ -178,14 +178,14 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
     typedef Kv4<D> L;
     constexpr int BC = 32 * NW, KS = D / 16, VT = D / 32, T = (D < 128 ? D : 128) / 16;
     __shared__ Tiles<D> tiles[NB];
-    __shared__ PlanSpace space;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5;
     const int worker = blockIdx.x;
-    Walk walk = find_share<BC, 64 * NW>(a.s, a.workers, worker, kTiledShare, space);
+    Walk walk = find_share<BC, true>(a.s, a.workers, worker, kTiledShare);
     int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
         const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
         const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
+        if (left_to_next(a.s, walk, t, take)) break;
         int p0, p1;
         pages_of(a.s, t, walk.at, take, p0, p1);
         const int cc = walk.j * BC + wave * 32 + (lane & 31), i = cc / a.s.group;
@@ -367,12 +367,7 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
         const bool whole = walk.at == 0 && take == t.cost;
         const int64_t slot = 2 * worker + (first ? 0 : 1);
         if (walk.at == 0 && !whole) {
-            const int rest = t.cost - take;
-            join[0] = 1 + (int)((rest + walk.share - 1) / walk.share);
-            join[1] = walk.b;
-            join[2] = walk.j;
-            join[3] = walk.h;
-            join[4] = (int)slot;
+            set_join(join, walk, t, BC, take, (int)slot);
         }
         if (live) {
             l += swapped_halves(l, lane);
@@ -405,7 +400,7 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
                 } else if (a.lse) a.lse[row] = l == 0 ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
             }
         }
-        advance<BC>(a.s, walk, t, take);
+        advance<BC, true>(a.s, walk, t, take);
     }
     if (threadIdx.x < 8) {
         int v = join[0];
