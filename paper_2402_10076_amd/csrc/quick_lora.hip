@@ -13,7 +13,8 @@ typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kMaxE = QUICK_MAX_EXPERTS;
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;       // of the second product
+constexpr int kDownThreads = 512;   // of the first
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -123,61 +124,67 @@ struct RowTile {
 
 __device__ __forceinline__ int clamped(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 
-// The workgroup's tile of H rows, the index'th of all: the first wave adds the
-// adapters' tiles up, eight to a lane (and the rows without one).
-template <int H>
-__device__ __forceinline__ RowTile find_tile(const LoraArgs& a, int index, int (&space)[3])
+// Rows of class e of the order: of adapter e, or (e == E) those without one.
+__device__ __forceinline__ int rows_of(const LoraArgs& a, int e, int& first)
 {
-    constexpr int PER = kMaxE / 64;
-    if (threadIdx.x < 64) {
-        const int lane = threadIdx.x;
-        int first[PER + 1], n[PER + 1], sum = 0;
-#pragma unroll
-        for (int i = 0; i <= PER; i++) {
-            // the last lane also has the rows without an adapter
-            const int e = i < PER ? lane * PER + i : lane == 63 ? a.E : a.E + 1;
-            first[i] = n[i] = 0;
-            if (e <= a.E) {
-                first[i] = clamped(a.offsets[e], 0, a.R);
-                const int end = e < a.E ? clamped(a.offsets[e + 1], first[i], a.R) : a.R;
-                n[i] = i < PER && e == a.E ? 0 : end - first[i];
-            }
-            sum += (n[i] + H - 1) / H;
-        }
-        int upto = sum;
-        for (int d = 1; d < 64; d *= 2) {
-            const int o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
-        if (lane == 63 && index >= upto) space[2] = 0;
-        int at = upto - sum;
-        if (index >= at && index < upto) {
-#pragma unroll
-            for (int i = 0; i <= PER; i++) {
-                const int tiles = (n[i] + H - 1) / H;
-                if (index >= at && index < at + tiles) {
-                    space[0] = i < PER ? lane * PER + i : a.E;
-                    space[1] = first[i] + (index - at) * H;
-                    space[2] = min(H, n[i] - (index - at) * H);
-                }
-                at += tiles;
-            }
-        }
-    }
-    __syncthreads();
-    return {(int)uniform((uint32_t)space[0]), (int)uniform((uint32_t)space[1]), (int)uniform((uint32_t)space[2])};
+    first = clamped(a.offsets[e], 0, a.R);
+    return (e < a.E ? clamped(a.offsets[e + 1], first, a.R) : a.R) - first;
 }
 
-// low = x . A^T of a tile of 16 TM rows and a slice of the channels.  Waves take
-// every fourth 128 channels; the rows of A (16 RT of them) are the instruction's
-// rows, those of x its columns, both straight from memory, 16 bytes a lane; the
-// waves' sums meet in LDS.
-template <int DT, int RT, int TM>
-__global__ __launch_bounds__(kThreads) void lora_down_kernel(LoraArgs a)
+// Inclusive sums over the lanes of a wave.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_from(int v)
 {
-    __shared__ int space[3];
-    __shared__ float sums[4][16][16 * RT + 4];
-    const RowTile t = find_tile<16 * TM>(a, blockIdx.x, space);
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
+}
+__device__ __forceinline__ int sums_upto(int v)
+{
+    v = add_from<0x111, 0xF>(v);
+    v = add_from<0x112, 0xF>(v);
+    v = add_from<0x114, 0xF>(v);
+    v = add_from<0x118, 0xF>(v);
+    v = add_from<0x142, 0xA>(v);
+    return add_from<0x143, 0xC>(v);
+}
+
+// The index'th tile of H rows of all.  Every wave works it out by itself, its
+// lanes adding up the tiles of the classes.
+template <int H>
+__device__ __forceinline__ RowTile find_tile(const LoraArgs& a, int index)
+{
+    const int lane = threadIdx.x & 63, per = (a.E + 64) / 64;    // classes of a lane
+    int sum = 0, first;
+    for (int e = lane * per; e < min((lane + 1) * per, a.E + 1); e++) sum += (rows_of(a, e, first) + H - 1) / H;
+    const int upto = sums_upto(sum);
+    RowTile t{0, 0, 0};
+    const uint64_t m = __ballot(upto > index);
+    if (!m) return t;
+    const int from = __builtin_ctzll(m);
+    if (lane == from) {
+        int at = upto - sum;
+        for (int e = lane * per; e < min((lane + 1) * per, a.E + 1); e++) {
+            const int n = rows_of(a, e, first), tiles = (n + H - 1) / H;
+            if (index < at + tiles) {
+                t = RowTile{e, first + (index - at) * H, min(H, n - (index - at) * H)};
+                break;
+            }
+            at += tiles;
+        }
+    }
+    return {__builtin_amdgcn_readlane(t.e, from), __builtin_amdgcn_readlane(t.first, from),
+            __builtin_amdgcn_readlane(t.count, from)};
+}
+
+// low = x . A^T of a tile of 16 TM rows and a slice of the channels.  Each of
+// eight waves takes every eighth 128 channels; the rows of A (16 RT of them) are
+// the instruction's rows, those of x its columns, both straight from memory, 16
+// bytes a lane; the waves' sums meet in LDS.
+template <int DT, int RT, int TM>
+__global__ __launch_bounds__(kDownThreads, RT * TM > 16 ? 1 : 2) void lora_down_kernel(LoraArgs a)
+{
+    constexpr int WAVES = kDownThreads / 64;
+    __shared__ float sums[WAVES][16][16 * RT + 4];
+    const RowTile t = find_tile<16 * TM>(a, blockIdx.x);
     if (t.count == 0 || t.e == a.E) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
     const int k0 = blockIdx.y * a.slice, k1 = min(a.K, k0 + a.slice);
@@ -196,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void lora_down_kernel(LoraArgs a)
     for (int m = 0; m < TM; m++)
 #pragma unroll
         for (int r = 0; r < RT; r++) acc[m][r] = f4_t{0, 0, 0, 0};
-    for (int k = k0 + wave * 128; k < k1; k += 512) {
+    for (int k = k0 + wave * 128; k < k1; k += WAVES * 128) {
 #pragma unroll
         for (int s = 0; s < 4; s++) {
             const int at = k + s * 32 + g * 8;
@@ -219,111 +226,135 @@ __global__ __launch_bounds__(kThreads) void lora_down_kernel(LoraArgs a)
     }
 #pragma unroll
     for (int m = 0; m < TM; m++) {
-        __syncthreads();
+        if (m) __syncthreads();
 #pragma unroll
         for (int r = 0; r < RT; r++) *(f4_t*)&sums[wave][c][r * 16 + g * 4] = acc[m][r];
         __syncthreads();
-        for (int i = threadIdx.x; i < 16 * 16 * RT; i += kThreads) {
-            const int row = i / (16 * RT), r = i % (16 * RT);
-            if (m * 16 + row < t.count && r < a.rank)
-                a.low[((int64_t)blockIdx.y * a.R + t.first + m * 16 + row) * a.rank + r] =
-                    sums[0][row][r] + sums[1][row][r] + sums[2][row][r] + sums[3][row][r];
+        // four columns a thread (the rank is a multiple of eight)
+        for (int i = threadIdx.x; i < 16 * 4 * RT; i += kDownThreads) {
+            const int row = i / (4 * RT), r = i % (4 * RT) * 4;
+            if (m * 16 + row >= t.count || r >= a.rank) continue;
+            f4_t v = *(const f4_t*)&sums[0][row][r];
+#pragma unroll
+            for (int n = 1; n < WAVES; n++) v += *(const f4_t*)&sums[n][row][r];
+            *(f4_t*)(a.low + ((int64_t)blockIdx.y * a.R + t.first + m * 16 + row) * a.rank + r) = v;
         }
     }
 }
 
-// out = y + low . B^T of a tile of 16 TM rows and 256 columns, 64 a wave.  The
+// out = y + low . B^T of a tile of 16 TM rows, 64 columns a wave at a time.  The
 // rows of B are the instruction's rows, in an order that leaves a lane 16
 // consecutive columns of its token: row 4 g + i of tile j is column 16 g + 4 j +
-// i.  With a rank of 8 or 16 a lane group's 16 bytes are of another tile (or of
-// two), and both operands are zero but for that group's lanes, so that every
-// load is full.
+// i.  The sums of low over the slices, scaled and rounded, are the other operand
+// and stay in registers for all columns.  With a rank of 8 or 16 a lane group's
+// 16 bytes of B are of another tile (or of two), and both operands are zero but
+// for that group's lanes, so that every load is full.
+// Bound by the bytes of y and out for many rows.
 template <int DT, int RS, int TM>
-__global__ __launch_bounds__(kThreads) void lora_up_kernel(LoraArgs a)
+__global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
 {
-    // RS: the rank's steps of 32 (0: rank 8 or 16)
-    constexpr int R32 = RS ? RS * 32 : 32, ROW = R32 + 8;
-    __shared__ int space[3];
-    __shared__ __align__(16) uint16_t low[16 * TM][ROW];
-    const RowTile t = find_tile<16 * TM>(a, blockIdx.x, space);
+    constexpr int STEPS = RS ? RS : 1;      // of 32 ranks (RS == 0: rank 8 or 16)
+    const RowTile t = find_tile<16 * TM>(a, blockIdx.x);
     if (t.count == 0) return;
     const bool bare = t.e == a.E;
     if (bare && a.out == a.y) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.y * 256 + wave * 64;
-    f4_t acc[TM][4];
-#pragma unroll
-    for (int m = 0; m < TM; m++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) acc[m][j] = f4_t{0, 0, 0, 0};
-    if (!bare) {
-        const float scale = a.scales ? a.scales[t.e] : 1.0f;
-        for (int i = threadIdx.x; i < 16 * TM * R32; i += kThreads) {
-            const int row = i / R32, r = i % R32;
-            float v = 0;
-            if (row < t.count && r < a.rank)
-                for (int s = 0; s < a.slices; s++) v += a.low[((int64_t)s * a.R + t.first + row) * a.rank + r];
-            low[row][r] = to16<DT>(v * scale);
-        }
-        __syncthreads();
-        const uint8_t* b = a.b + 2 * (int64_t)t.e * a.N * a.rank;
-        // column of this lane's row of tile j
-        auto column = [&](int j) { return n0 + (c >> 2) * 16 + j * 4 + (c & 3); };
-        if constexpr (RS == 0) {
-            // 2 or 4 tiles of one load
-            const int per = 32 / a.rank, mine = g * 8 / a.rank, r = g * 8 % a.rank;
-            for (int j0 = 0; j0 < 4; j0 += per) {
-                const int n = column(j0 + mine);
-                u4_t w = {0, 0, 0, 0};
-                if (n < a.N) w = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + r));
-#pragma unroll
-                for (int m = 0; m < TM; m++) {
-                    const u4_t v = *(const u4_t*)&low[m * 16 + c][r];
-#pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        if (j >= j0 && j < j0 + per)
-                            acc[m][j] = mfma16<DT>(mine == j - j0 ? w : u4_t{0, 0, 0, 0},
-                                                   mine == j - j0 ? v : u4_t{0, 0, 0, 0}, acc[m][j]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < RS; s++) {
-                u4_t w[4];
-                const int r = s * 32 + g * 8;
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const int n = column(j);
-                    w[j] = u4_t{0, 0, 0, 0};
-                    if (n < a.N && r < a.rank) w[j] = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + r));
-                }
-#pragma unroll
-                for (int m = 0; m < TM; m++) {
-                    const u4_t v = *(const u4_t*)&low[m * 16 + c][r];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) acc[m][j] = mfma16<DT>(w[j], v, acc[m][j]);
-                }
-            }
-        }
-    }
+    int row[TM];
 #pragma unroll
     for (int m = 0; m < TM; m++) {
         const int at = m * 16 + c;
-        const int row = at < t.count ? a.rows[t.first + at] : -1;
-        if (row < 0 || row >= a.T) continue;
+        row[m] = at < t.count ? a.rows[t.first + at] : -1;
+        if (row[m] >= a.T) row[m] = -1;
+    }
+    // with a low rank every lane group holds the same of it (8 g % rank)
+    const int per = RS ? 1 : 32 / a.rank, mine = RS ? 0 : g * 8 / a.rank;
+    u4_t low[STEPS][TM];
+    const float scale = !bare && a.scales ? a.scales[t.e] : 1.0f;
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int n = n0 + g * 16 + h * 8;
-            if (n >= a.N) continue;
-            const u4_t y = *(const u4_t*)(a.y + 2 * ((int64_t)row * a.ldy + n));
-            u4_t o;
+    for (int s = 0; s < STEPS; s++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const f4_t v = acc[m][h * 2 + i / 2];
-                o[i] = to16x2<DT>(from16<DT>((uint16_t)y[i]) + v[i % 2 * 2], from16<DT>((uint16_t)(y[i] >> 16)) + v[i % 2 * 2 + 1]);
+        for (int m = 0; m < TM; m++) {
+            const int r = RS ? s * 32 + g * 8 : g * 8 % a.rank;
+            f4_t u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+            if (!bare && m * 16 + c < t.count && r < a.rank) {
+                const float* from = a.low + (int64_t)(t.first + m * 16 + c) * a.rank + r;
+#pragma unroll 4
+                for (int n = 0; n < a.slices; n++) {
+                    u += *(const f4_t*)(from + (int64_t)n * a.R * a.rank);
+                    v += *(const f4_t*)(from + (int64_t)n * a.R * a.rank + 4);
+                }
             }
-            *(u4_t*)(a.out + 2 * ((int64_t)row * a.ldo + n)) = bare ? y : o;
+            u *= scale;
+            v *= scale;
+            low[s][m] = u4_t{to16x2<DT>(u[0], u[1]), to16x2<DT>(u[2], u[3]), to16x2<DT>(v[0], v[1]), to16x2<DT>(v[2], v[3])};
         }
+    const uint8_t* b = a.b + 2 * (int64_t)(bare ? 0 : t.e) * a.N * a.rank;
+    for (int n0 = (blockIdx.y * 4 + wave) * 64; n0 < a.N; n0 += gridDim.y * 256) {
+        u4_t y[TM][2];
+#pragma unroll
+        for (int m = 0; m < TM; m++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int n = n0 + g * 16 + h * 8;
+                y[m][h] = u4_t{0, 0, 0, 0};
+                if (row[m] >= 0 && n < a.N) y[m][h] = *(const u4_t*)(a.y + 2 * ((int64_t)row[m] * a.ldy + n));
+            }
+        f4_t acc[TM][4];
+#pragma unroll
+        for (int m = 0; m < TM; m++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[m][j] = f4_t{0, 0, 0, 0};
+        if (!bare) {
+            // column of this lane's row of tile j
+            auto column = [&](int j) { return n0 + (c >> 2) * 16 + j * 4 + (c & 3); };
+            if constexpr (RS == 0) {
+                const int r = g * 8 % a.rank;
+                for (int j0 = 0; j0 < 4; j0 += per) {
+                    const int n = column(j0 + mine);
+                    u4_t w = {0, 0, 0, 0};
+                    if (n < a.N) w = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + r));
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        if (j < j0 || j >= j0 + per) continue;
+                        const bool here = mine == j - j0;
+#pragma unroll
+                        for (int m = 0; m < TM; m++)
+                            acc[m][j] = mfma16<DT>(here ? w : u4_t{0, 0, 0, 0}, here ? low[0][m] : u4_t{0, 0, 0, 0}, acc[m][j]);
+                    }
+                }
+            } else {
+                u4_t w[STEPS][4];
+#pragma unroll
+                for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const int n = column(j), r = s * 32 + g * 8;
+                        w[s][j] = u4_t{0, 0, 0, 0};
+                        if (n < a.N && r < a.rank) w[s][j] = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + r));
+                    }
+#pragma unroll
+                for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                    for (int m = 0; m < TM; m++)
+#pragma unroll
+                        for (int j = 0; j < 4; j++) acc[m][j] = mfma16<DT>(w[s][j], low[s][m], acc[m][j]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < TM; m++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int n = n0 + g * 16 + h * 8;
+                if (row[m] < 0 || n >= a.N) continue;
+                u4_t o;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const f4_t v = acc[m][h * 2 + i / 2];
+                    o[i] = to16x2<DT>(from16<DT>((uint16_t)y[m][h][i]) + v[i % 2 * 2],
+                                      from16<DT>((uint16_t)(y[m][h][i] >> 16)) + v[i % 2 * 2 + 1]);
+                }
+                *(u4_t*)(a.out + 2 * ((int64_t)row[m] * a.ldo + n)) = bare ? y[m][h] : o;
+            }
     }
 }
 
@@ -337,10 +368,11 @@ int64_t tiles_of(int64_t R, int64_t E)
     return R / h + std::min(E + 1, R);
 }
 
-// Slices of the channels: enough workgroups for the chip, 512 channels or more.
+// Slices of the channels: a workgroup for each compute unit, 1024 channels or
+// more (128 a wave).
 void slices_of(int64_t R, int64_t K, int64_t E, int32_t* slices, int32_t* slice)
 {
-    const int64_t n = std::max<int64_t>(1, std::min(ceil_div(K, 512), 512 / tiles_of(R, E)));
+    const int64_t n = std::max<int64_t>(1, std::min(ceil_div(K, 1024), 320 / tiles_of(R, E)));
     *slice = (int32_t)(ceil_div(ceil_div(K, n), 128) * 128);
     *slices = (int32_t)ceil_div(K, *slice);
 }
@@ -349,11 +381,13 @@ template <int DT, int TM>
 void launch_lora(const LoraArgs& a, hipStream_t hs)
 {
     const uint32_t tiles = (uint32_t)tiles_of(a.R, a.E);
-    const dim3 down(tiles, a.slices), up(tiles, (uint32_t)ceil_div(a.N, 256));
-    if (a.rank <= 16) lora_down_kernel<DT, 1, TM><<<down, kThreads, 0, hs>>>(a);
-    else if (a.rank <= 32) lora_down_kernel<DT, 2, TM><<<down, kThreads, 0, hs>>>(a);
-    else if (a.rank <= 64) lora_down_kernel<DT, 4, TM><<<down, kThreads, 0, hs>>>(a);
-    else lora_down_kernel<DT, 8, TM><<<down, kThreads, 0, hs>>>(a);
+    // columns: enough workgroups for the chip, and no more, as each begins with the sums over the slices
+    const int64_t most = ceil_div(a.N, 256), want = ceil_div(1024, tiles);
+    const dim3 down(tiles, a.slices), up(tiles, (uint32_t)std::min(most, want));
+    if (a.rank <= 16) lora_down_kernel<DT, 1, TM><<<down, kDownThreads, 0, hs>>>(a);
+    else if (a.rank <= 32) lora_down_kernel<DT, 2, TM><<<down, kDownThreads, 0, hs>>>(a);
+    else if (a.rank <= 64) lora_down_kernel<DT, 4, TM><<<down, kDownThreads, 0, hs>>>(a);
+    else lora_down_kernel<DT, 8, TM><<<down, kDownThreads, 0, hs>>>(a);
     if (a.rank == 8 || a.rank == 16) lora_up_kernel<DT, 0, TM><<<up, kThreads, 0, hs>>>(a);
     else if (a.rank <= 32) lora_up_kernel<DT, 1, TM><<<up, kThreads, 0, hs>>>(a);
     else if (a.rank <= 64) lora_up_kernel<DT, 2, TM><<<up, kThreads, 0, hs>>>(a);
