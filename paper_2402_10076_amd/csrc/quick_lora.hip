@@ -180,7 +180,7 @@ __device__ __forceinline__ RowTile find_tile(const LoraArgs& a, int index)
 // the instruction's rows, those of x its columns, both straight from memory, 16
 // bytes a lane; the waves' sums meet in LDS.
 template <int DT, int RT, int TM>
-__global__ __launch_bounds__(kDownThreads, RT * TM > 16 ? 1 : 2) void lora_down_kernel(LoraArgs a)
+__global__ __launch_bounds__(kDownThreads, RT * TM > 8 ? 2 : 4) void lora_down_kernel(LoraArgs a)
 {
     constexpr int WAVES = kDownThreads / 64;
     __shared__ float sums[WAVES][16][16 * RT + 4];
@@ -188,41 +188,56 @@ __global__ __launch_bounds__(kDownThreads, RT * TM > 16 ? 1 : 2) void lora_down_
     if (t.count == 0 || t.e == a.E) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
     const int k0 = blockIdx.y * a.slice, k1 = min(a.K, k0 + a.slice);
+    // (lanes without a row, or behind the rank, read another one, and their sums go nowhere)
     const uint8_t* x[TM];
-    bool live[TM];
 #pragma unroll
     for (int m = 0; m < TM; m++) {
-        const int at = m * 16 + c;
-        const int row = at < t.count ? a.rows[t.first + at] : -1;
-        live[m] = row >= 0 && row < a.T;
-        x[m] = a.x + 2 * ((int64_t)(live[m] ? row : 0) * a.ldx);
+        const int row = a.rows[t.first + min(m * 16 + c, t.count - 1)];
+        x[m] = a.x + 2 * ((int64_t)(row >= 0 && row < a.T ? row : 0) * a.ldx + g * 8);
     }
-    const uint8_t* w = a.a + 2 * (int64_t)t.e * a.rank * a.K;
+    const uint8_t* w[RT];
+#pragma unroll
+    for (int r = 0; r < RT; r++)
+        w[r] = a.a + 2 * (((int64_t)t.e * a.rank + min(r * 16 + c, a.rank - 1)) * a.K + g * 8);
     f4_t acc[TM][RT];
 #pragma unroll
     for (int m = 0; m < TM; m++)
 #pragma unroll
         for (int r = 0; r < RT; r++) acc[m][r] = f4_t{0, 0, 0, 0};
     for (int k = k0 + wave * 128; k < k1; k += WAVES * 128) {
+        u4_t xv[4][TM], wv[4][RT];
+        if (k + 128 <= k1) {
 #pragma unroll
-        for (int s = 0; s < 4; s++) {
-            const int at = k + s * 32 + g * 8;
-            u4_t xv[TM], wv[RT];
+            for (int s = 0; s < 4; s++) {
 #pragma unroll
-            for (int m = 0; m < TM; m++) {
-                xv[m] = u4_t{0, 0, 0, 0};
-                if (at < k1 && live[m]) xv[m] = *(const u4_t*)(x[m] + 2 * at);
+                for (int m = 0; m < TM; m++) xv[s][m] = *(const u4_t*)(x[m] + 2 * (k + s * 32));
+#pragma unroll
+                for (int r = 0; r < RT; r++) wv[s][r] = *(const u4_t*)(w[r] + 2 * (k + s * 32));
             }
+        } else {
+            // the last channels: eights behind the end are zero in both
 #pragma unroll
-            for (int r = 0; r < RT; r++) {
-                wv[r] = u4_t{0, 0, 0, 0};
-                if (at < k1 && r * 16 + c < a.rank) wv[r] = *(const u4_t*)(w + 2 * ((int64_t)(r * 16 + c) * a.K + at));
+            for (int s = 0; s < 4; s++) {
+                const bool in = k + s * 32 + g * 8 < k1;
+                const int at = in ? k + s * 32 : k0 - g * 8;
+#pragma unroll
+                for (int m = 0; m < TM; m++) {
+                    const u4_t v = *(const u4_t*)(x[m] + 2 * (int64_t)at);
+                    xv[s][m] = in ? v : u4_t{0, 0, 0, 0};
+                }
+#pragma unroll
+                for (int r = 0; r < RT; r++) {
+                    const u4_t v = *(const u4_t*)(w[r] + 2 * (int64_t)at);
+                    wv[s][r] = in ? v : u4_t{0, 0, 0, 0};
+                }
             }
+        }
+#pragma unroll
+        for (int s = 0; s < 4; s++)
 #pragma unroll
             for (int m = 0; m < TM; m++)
 #pragma unroll
-                for (int r = 0; r < RT; r++) acc[m][r] = mfma16<DT>(wv[r], xv[m], acc[m][r]);
-        }
+                for (int r = 0; r < RT; r++) acc[m][r] = mfma16<DT>(wv[s][r], xv[s][m], acc[m][r]);
     }
 #pragma unroll
     for (int m = 0; m < TM; m++) {
@@ -243,9 +258,9 @@ __global__ __launch_bounds__(kDownThreads, RT * TM > 16 ? 1 : 2) void lora_down_
 }
 
 // out = y + low . B^T of a tile of 16 TM rows, 64 columns a wave at a time.  The
-// rows of B are the instruction's rows, in an order that leaves a lane 16
-// consecutive columns of its token: row 4 g + i of tile j is column 16 g + 4 j +
-// i.  The sums of low over the slices, scaled and rounded, are the other operand
+// rows of B are the instruction's rows, in an order that leaves a lane twice 8
+// consecutive columns of its token, and four lanes 64 bytes: row 4 g + i of tile
+// j is column 32 (j / 2) + 8 g + 4 (j % 2) + i.  The sums of low over the slices, scaled and rounded, are the other operand
 // and stay in registers for all columns.  With a rank of 8 or 16 a lane group's
 // 16 bytes of B are of another tile (or of two), and both operands are zero but
 // for that group's lanes, so that every load is full.
@@ -254,97 +269,100 @@ template <int DT, int RS, int TM>
 __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
 {
     constexpr int STEPS = RS ? RS : 1;      // of 32 ranks (RS == 0: rank 8 or 16)
-    const RowTile t = find_tile<16 * TM>(a, blockIdx.x);
+    const RowTile t = find_tile<16 * TM>(a, blockIdx.y);
     if (t.count == 0) return;
     const bool bare = t.e == a.E;
     if (bare && a.out == a.y) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    // (what is behind the rows, the columns or the rank is read from another place and goes nowhere)
     int row[TM];
+    const uint8_t* ys[TM];
 #pragma unroll
     for (int m = 0; m < TM; m++) {
-        const int at = m * 16 + c;
-        row[m] = at < t.count ? a.rows[t.first + at] : -1;
-        if (row[m] >= a.T) row[m] = -1;
+        const int at = m * 16 + c, x = a.rows[t.first + min(at, t.count - 1)];
+        row[m] = at < t.count && x >= 0 && x < a.T ? x : -1;
+        ys[m] = a.y + 2 * ((int64_t)max(row[m], 0) * a.ldy);
     }
     // with a low rank every lane group holds the same of it (8 g % rank)
     const int per = RS ? 1 : 32 / a.rank, mine = RS ? 0 : g * 8 / a.rank;
     u4_t low[STEPS][TM];
     const float scale = !bare && a.scales ? a.scales[t.e] : 1.0f;
+    if (!bare) {
 #pragma unroll
-    for (int s = 0; s < STEPS; s++)
+        for (int s = 0; s < STEPS; s++)
 #pragma unroll
-        for (int m = 0; m < TM; m++) {
-            const int r = RS ? s * 32 + g * 8 : g * 8 % a.rank;
-            f4_t u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-            if (!bare && m * 16 + c < t.count && r < a.rank) {
-                const float* from = a.low + (int64_t)(t.first + m * 16 + c) * a.rank + r;
+            for (int m = 0; m < TM; m++) {
+                const int r = RS ? s * 32 + g * 8 : g * 8 % a.rank;
+                f4_t u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+                const float* from = a.low + (int64_t)(t.first + min(m * 16 + c, t.count - 1)) * a.rank + min(r, a.rank - 8);
 #pragma unroll 4
                 for (int n = 0; n < a.slices; n++) {
                     u += *(const f4_t*)(from + (int64_t)n * a.R * a.rank);
                     v += *(const f4_t*)(from + (int64_t)n * a.R * a.rank + 4);
                 }
+                u *= scale;
+                v *= scale;
+                low[s][m] = u4_t{to16x2<DT>(u[0], u[1]), to16x2<DT>(u[2], u[3]), to16x2<DT>(v[0], v[1]), to16x2<DT>(v[2], v[3])};
+                if (r >= a.rank) low[s][m] = u4_t{0, 0, 0, 0};
             }
-            u *= scale;
-            v *= scale;
-            low[s][m] = u4_t{to16x2<DT>(u[0], u[1]), to16x2<DT>(u[2], u[3]), to16x2<DT>(v[0], v[1]), to16x2<DT>(v[2], v[3])};
-        }
+    }
     const uint8_t* b = a.b + 2 * (int64_t)(bare ? 0 : t.e) * a.N * a.rank;
-    for (int n0 = (blockIdx.y * 4 + wave) * 64; n0 < a.N; n0 += gridDim.y * 256) {
-        u4_t y[TM][2];
+    u4_t w[STEPS][4], y[TM][2];
+    auto load_b = [&](int n0) {
+        if (bare) return;
+#pragma unroll
+        for (int s = 0; s < STEPS; s++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                // with a low rank load j is that of tiles per * j .. per * j + per - 1
+                if (per * j >= 4) continue;
+                const int tile = RS ? j : per * j + mine, r = RS ? s * 32 + g * 8 : g * 8 % a.rank;
+                const int n = min(n0 + (tile >> 1) * 32 + (c >> 2) * 8 + (tile & 1) * 4 + (c & 3), a.N - 1);
+                w[s][j] = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + min(r, a.rank - 8)));
+                if (RS && s == STEPS - 1 && r >= a.rank) w[s][j] = u4_t{0, 0, 0, 0};
+            }
+    };
+    auto load_y = [&](int n0) {
 #pragma unroll
         for (int m = 0; m < TM; m++)
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int n = n0 + g * 16 + h * 8;
-                y[m][h] = u4_t{0, 0, 0, 0};
-                if (row[m] >= 0 && n < a.N) y[m][h] = *(const u4_t*)(a.y + 2 * ((int64_t)row[m] * a.ldy + n));
-            }
+            for (int h = 0; h < 2; h++) y[m][h] = *(const u4_t*)(ys[m] + 2 * min(n0 + h * 32 + g * 8, a.N - 8));
+    };
+    const int step = gridDim.x * 256;
+    int n0 = (blockIdx.x * 4 + wave) * 64;
+    load_b(n0);
+    load_y(n0);
+    for (; n0 < a.N; n0 += step) {
         f4_t acc[TM][4];
 #pragma unroll
         for (int m = 0; m < TM; m++)
 #pragma unroll
             for (int j = 0; j < 4; j++) acc[m][j] = f4_t{0, 0, 0, 0};
-        if (!bare) {
-            // column of this lane's row of tile j
-            auto column = [&](int j) { return n0 + (c >> 2) * 16 + j * 4 + (c & 3); };
-            if constexpr (RS == 0) {
-                const int r = g * 8 % a.rank;
-                for (int j0 = 0; j0 < 4; j0 += per) {
-                    const int n = column(j0 + mine);
-                    u4_t w = {0, 0, 0, 0};
-                    if (n < a.N) w = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + r));
+        if (bare) {
+        } else if constexpr (RS == 0) {
 #pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        if (j < j0 || j >= j0 + per) continue;
-                        const bool here = mine == j - j0;
+            for (int j = 0; j < 4; j++) {
+                const bool here = mine == j % per;
+                const u4_t v = per == 4 ? w[0][0] : w[0][j / 2];
 #pragma unroll
-                        for (int m = 0; m < TM; m++)
-                            acc[m][j] = mfma16<DT>(here ? w : u4_t{0, 0, 0, 0}, here ? low[0][m] : u4_t{0, 0, 0, 0}, acc[m][j]);
-                    }
-                }
-            } else {
-                u4_t w[STEPS][4];
-#pragma unroll
-                for (int s = 0; s < STEPS; s++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const int n = column(j), r = s * 32 + g * 8;
-                        w[s][j] = u4_t{0, 0, 0, 0};
-                        if (n < a.N && r < a.rank) w[s][j] = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + r));
-                    }
-#pragma unroll
-                for (int s = 0; s < STEPS; s++)
-#pragma unroll
-                    for (int m = 0; m < TM; m++)
-#pragma unroll
-                        for (int j = 0; j < 4; j++) acc[m][j] = mfma16<DT>(w[s][j], low[s][m], acc[m][j]);
+                for (int m = 0; m < TM; m++)
+                    acc[m][j] = mfma16<DT>(here ? v : u4_t{0, 0, 0, 0}, here ? low[0][m] : u4_t{0, 0, 0, 0}, acc[m][j]);
             }
+        } else {
+#pragma unroll
+            for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                for (int m = 0; m < TM; m++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) acc[m][j] = mfma16<DT>(w[s][j], low[s][m], acc[m][j]);
         }
+        // the next columns' operands take the place of these as they are done with
+        load_b(n0 + step);
 #pragma unroll
         for (int m = 0; m < TM; m++)
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const int n = n0 + g * 16 + h * 8;
+                const int n = n0 + h * 32 + g * 8;
                 if (row[m] < 0 || n >= a.N) continue;
                 u4_t o;
 #pragma unroll
@@ -355,6 +373,7 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
                 }
                 *(u4_t*)(a.out + 2 * ((int64_t)row[m] * a.ldo + n)) = bare ? y[m][h] : o;
             }
+        load_y(n0 + step);
     }
 }
 
@@ -368,12 +387,12 @@ int64_t tiles_of(int64_t R, int64_t E)
     return R / h + std::min(E + 1, R);
 }
 
-// Slices of the channels: a workgroup for each compute unit, 1024 channels or
-// more (128 a wave).
+// Slices of the channels: a workgroup for each compute unit and some more, whole
+// rounds of its waves (1024 channels).
 void slices_of(int64_t R, int64_t K, int64_t E, int32_t* slices, int32_t* slice)
 {
-    const int64_t n = std::max<int64_t>(1, std::min(ceil_div(K, 1024), 320 / tiles_of(R, E)));
-    *slice = (int32_t)(ceil_div(ceil_div(K, n), 128) * 128);
+    const int64_t rounds = ceil_div(K, 1024), n = std::max<int64_t>(1, std::min(rounds, 320 / tiles_of(R, E)));
+    *slice = (int32_t)(ceil_div(rounds, n) * 1024);
     *slices = (int32_t)ceil_div(K, *slice);
 }
 
@@ -381,9 +400,11 @@ template <int DT, int TM>
 void launch_lora(const LoraArgs& a, hipStream_t hs)
 {
     const uint32_t tiles = (uint32_t)tiles_of(a.R, a.E);
-    // columns: enough workgroups for the chip, and no more, as each begins with the sums over the slices
-    const int64_t most = ceil_div(a.N, 256), want = ceil_div(1024, tiles);
-    const dim3 down(tiles, a.slices), up(tiles, (uint32_t)std::min(most, want));
+    // columns: enough workgroups for the chip, and no more, as each begins with the sums over the slices; those of one
+    // eighth follow each other eight apart, on one die, whose cache then holds their part of B (15360 columns of rank
+    // 64 of four adapters: 42 us, 86 with the tiles on the dies)
+    const int64_t most = ceil_div(a.N, 256), want = ceil_div(ceil_div(512, tiles), 8) * 8;
+    const dim3 down(tiles, a.slices), up((uint32_t)std::min(most, want), tiles);
     if (a.rank <= 16) lora_down_kernel<DT, 1, TM><<<down, kDownThreads, 0, hs>>>(a);
     else if (a.rank <= 32) lora_down_kernel<DT, 2, TM><<<down, kDownThreads, 0, hs>>>(a);
     else if (a.rank <= 64) lora_down_kernel<DT, 4, TM><<<down, kDownThreads, 0, hs>>>(a);
