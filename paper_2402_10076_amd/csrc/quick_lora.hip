@@ -175,24 +175,28 @@ __device__ __forceinline__ RowTile find_tile(const LoraArgs& a, int index)
             __builtin_amdgcn_readlane(t.count, from)};
 }
 
-// low = x . A^T of a tile of 16 TM rows and a slice of the channels.  Each of
-// eight waves takes every eighth 128 channels; the rows of A (16 RT of them) are
-// the instruction's rows, those of x its columns, both straight from memory, 16
-// bytes a lane; the waves' sums meet in LDS.
-template <int DT, int RT, int TM>
-__global__ __launch_bounds__(kDownThreads, RT * TM > 8 ? 2 : 4) void lora_down_kernel(LoraArgs a)
+// low = x . A^T of a tile of 16 TM RW rows and a slice of the channels.  Of eight
+// waves RW share the rows out, 16 TM each, and the others the channels, each
+// taking 128 at a time; the rows of A (16 RT of them) are the instruction's
+// rows, those of x its columns, both straight from memory, 16 bytes a lane; the
+// waves' sums meet in LDS.  A tile is a chain of latencies: offsets, rows,
+// operands, LDS.
+template <int DT, int RT, int TM, int RW>
+__global__ __launch_bounds__(kDownThreads) void lora_down_kernel(LoraArgs a)
 {
-    constexpr int WAVES = kDownThreads / 64;
-    __shared__ float sums[WAVES][16][16 * RT + 4];
-    const RowTile t = find_tile<16 * TM>(a, blockIdx.x);
+    constexpr int KW = kDownThreads / 64 / RW, ROWS = 16 * TM * RW;
+    constexpr int STEPS = RT * TM > 8 ? 2 : 4;     // of 32 channels whose operands are loaded together
+    __shared__ float sums[KW][ROWS][16 * RT + 4];
+    const RowTile t = find_tile<ROWS>(a, blockIdx.x);
     if (t.count == 0 || t.e == a.E) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int row0 = wave % RW * 16 * TM, part = wave / RW;
     const int k0 = blockIdx.y * a.slice, k1 = min(a.K, k0 + a.slice);
     // (lanes without a row, or behind the rank, read another one, and their sums go nowhere)
     const uint8_t* x[TM];
 #pragma unroll
     for (int m = 0; m < TM; m++) {
-        const int row = a.rows[t.first + min(m * 16 + c, t.count - 1)];
+        const int row = a.rows[t.first + min(row0 + m * 16 + c, t.count - 1)];
         x[m] = a.x + 2 * ((int64_t)(row >= 0 && row < a.T ? row : 0) * a.ldx + g * 8);
     }
     const uint8_t* w[RT];
@@ -204,56 +208,59 @@ __global__ __launch_bounds__(kDownThreads, RT * TM > 8 ? 2 : 4) void lora_down_k
     for (int m = 0; m < TM; m++)
 #pragma unroll
         for (int r = 0; r < RT; r++) acc[m][r] = f4_t{0, 0, 0, 0};
-    for (int k = k0 + wave * 128; k < k1; k += WAVES * 128) {
-        u4_t xv[4][TM], wv[4][RT];
-        if (k + 128 <= k1) {
+    if (row0 < t.count) {
+        for (int k = k0 + part * 128; k < k1; k += KW * 128) {
 #pragma unroll
-            for (int s = 0; s < 4; s++) {
+            for (int s0 = 0; s0 < 4; s0 += STEPS) {
+                u4_t xv[STEPS][TM], wv[STEPS][RT];
+                if (k + 128 <= k1) {
 #pragma unroll
-                for (int m = 0; m < TM; m++) xv[s][m] = *(const u4_t*)(x[m] + 2 * (k + s * 32));
+                    for (int s = 0; s < STEPS; s++) {
 #pragma unroll
-                for (int r = 0; r < RT; r++) wv[s][r] = *(const u4_t*)(w[r] + 2 * (k + s * 32));
-            }
-        } else {
-            // the last channels: eights behind the end are zero in both
+                        for (int m = 0; m < TM; m++) xv[s][m] = *(const u4_t*)(x[m] + 2 * (k + (s0 + s) * 32));
 #pragma unroll
-            for (int s = 0; s < 4; s++) {
-                const bool in = k + s * 32 + g * 8 < k1;
-                const int at = in ? k + s * 32 : k0 - g * 8;
+                        for (int r = 0; r < RT; r++) wv[s][r] = *(const u4_t*)(w[r] + 2 * (k + (s0 + s) * 32));
+                    }
+                } else {
+                    // the last channels: eights behind the end are zero in both
 #pragma unroll
-                for (int m = 0; m < TM; m++) {
-                    const u4_t v = *(const u4_t*)(x[m] + 2 * (int64_t)at);
-                    xv[s][m] = in ? v : u4_t{0, 0, 0, 0};
+                    for (int s = 0; s < STEPS; s++) {
+                        const bool in = k + (s0 + s) * 32 + g * 8 < k1;
+                        const int64_t at = in ? k + (s0 + s) * 32 : k0 - g * 8;
+#pragma unroll
+                        for (int m = 0; m < TM; m++) {
+                            const u4_t v = *(const u4_t*)(x[m] + 2 * at);
+                            xv[s][m] = in ? v : u4_t{0, 0, 0, 0};
+                        }
+#pragma unroll
+                        for (int r = 0; r < RT; r++) {
+                            const u4_t v = *(const u4_t*)(w[r] + 2 * at);
+                            wv[s][r] = in ? v : u4_t{0, 0, 0, 0};
+                        }
+                    }
                 }
 #pragma unroll
-                for (int r = 0; r < RT; r++) {
-                    const u4_t v = *(const u4_t*)(w[r] + 2 * (int64_t)at);
-                    wv[s][r] = in ? v : u4_t{0, 0, 0, 0};
-                }
+                for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                    for (int m = 0; m < TM; m++)
+#pragma unroll
+                        for (int r = 0; r < RT; r++) acc[m][r] = mfma16<DT>(wv[s][r], xv[s][m], acc[m][r]);
             }
         }
 #pragma unroll
-        for (int s = 0; s < 4; s++)
+        for (int m = 0; m < TM; m++)
 #pragma unroll
-            for (int m = 0; m < TM; m++)
-#pragma unroll
-                for (int r = 0; r < RT; r++) acc[m][r] = mfma16<DT>(wv[s][r], xv[s][m], acc[m][r]);
+            for (int r = 0; r < RT; r++) *(f4_t*)&sums[part][row0 + m * 16 + c][r * 16 + g * 4] = acc[m][r];
     }
+    __syncthreads();
+    // four columns a thread (the rank is a multiple of eight)
+    for (int i = threadIdx.x; i < ROWS * 4 * RT; i += kDownThreads) {
+        const int row = i / (4 * RT), r = i % (4 * RT) * 4;
+        if (row >= t.count || r >= a.rank) continue;
+        f4_t v = *(const f4_t*)&sums[0][row][r];
 #pragma unroll
-    for (int m = 0; m < TM; m++) {
-        if (m) __syncthreads();
-#pragma unroll
-        for (int r = 0; r < RT; r++) *(f4_t*)&sums[wave][c][r * 16 + g * 4] = acc[m][r];
-        __syncthreads();
-        // four columns a thread (the rank is a multiple of eight)
-        for (int i = threadIdx.x; i < 16 * 4 * RT; i += kDownThreads) {
-            const int row = i / (4 * RT), r = i % (4 * RT) * 4;
-            if (m * 16 + row >= t.count || r >= a.rank) continue;
-            f4_t v = *(const f4_t*)&sums[0][row][r];
-#pragma unroll
-            for (int n = 1; n < WAVES; n++) v += *(const f4_t*)&sums[n][row][r];
-            *(f4_t*)(a.low + ((int64_t)blockIdx.y * a.R + t.first + m * 16 + row) * a.rank + r) = v;
-        }
+        for (int n = 1; n < KW; n++) v += *(const f4_t*)&sums[n][row][r];
+        *(f4_t*)(a.low + ((int64_t)blockIdx.y * a.R + t.first + row) * a.rank + r) = v;
     }
 }
 
@@ -288,22 +295,30 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
     u4_t low[STEPS][TM];
     const float scale = !bare && a.scales ? a.scales[t.e] : 1.0f;
     if (!bare) {
+        f4_t u[STEPS][TM], v[STEPS][TM];
+#pragma unroll
+        for (int s = 0; s < STEPS; s++)
+#pragma unroll
+            for (int m = 0; m < TM; m++) u[s][m] = v[s][m] = f4_t{0, 0, 0, 0};
+        // all of a slice's loads are under way together
+        for (int n = 0; n < a.slices; n++) {
+#pragma unroll
+            for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                for (int m = 0; m < TM; m++) {
+                    const int r = RS ? min(s * 32 + g * 8, a.rank - 8) : g * 8 % a.rank;
+                    const float* from = a.low + ((int64_t)n * a.R + t.first + min(m * 16 + c, t.count - 1)) * a.rank + r;
+                    u[s][m] += *(const f4_t*)from;
+                    v[s][m] += *(const f4_t*)(from + 4);
+                }
+        }
 #pragma unroll
         for (int s = 0; s < STEPS; s++)
 #pragma unroll
             for (int m = 0; m < TM; m++) {
-                const int r = RS ? s * 32 + g * 8 : g * 8 % a.rank;
-                f4_t u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-                const float* from = a.low + (int64_t)(t.first + min(m * 16 + c, t.count - 1)) * a.rank + min(r, a.rank - 8);
-#pragma unroll 4
-                for (int n = 0; n < a.slices; n++) {
-                    u += *(const f4_t*)(from + (int64_t)n * a.R * a.rank);
-                    v += *(const f4_t*)(from + (int64_t)n * a.R * a.rank + 4);
-                }
-                u *= scale;
-                v *= scale;
-                low[s][m] = u4_t{to16x2<DT>(u[0], u[1]), to16x2<DT>(u[2], u[3]), to16x2<DT>(v[0], v[1]), to16x2<DT>(v[2], v[3])};
-                if (r >= a.rank) low[s][m] = u4_t{0, 0, 0, 0};
+                const f4_t p = u[s][m] * scale, q = v[s][m] * scale;
+                low[s][m] = u4_t{to16x2<DT>(p[0], p[1]), to16x2<DT>(p[2], p[3]), to16x2<DT>(q[0], q[1]), to16x2<DT>(q[2], q[3])};
+                if (RS && s * 32 + g * 8 >= a.rank) low[s][m] = u4_t{0, 0, 0, 0};
             }
     }
     const uint8_t* b = a.b + 2 * (int64_t)(bare ? 0 : t.e) * a.N * a.rank;
@@ -405,10 +420,12 @@ void launch_lora(const LoraArgs& a, hipStream_t hs)
     // 64 of four adapters: 42 us, 86 with the tiles on the dies)
     const int64_t most = ceil_div(a.N, 256), want = ceil_div(ceil_div(512, tiles), 8) * 8;
     const dim3 down(tiles, a.slices), up((uint32_t)std::min(most, want), tiles);
-    if (a.rank <= 16) lora_down_kernel<DT, 1, TM><<<down, kDownThreads, 0, hs>>>(a);
-    else if (a.rank <= 32) lora_down_kernel<DT, 2, TM><<<down, kDownThreads, 0, hs>>>(a);
-    else if (a.rank <= 64) lora_down_kernel<DT, 4, TM><<<down, kDownThreads, 0, hs>>>(a);
-    else lora_down_kernel<DT, 8, TM><<<down, kDownThreads, 0, hs>>>(a);
+    // (LDS does not hold the sums of 128 ranks of 64 rows by eight waves)
+    constexpr int RW = TM > 1 ? 2 : 1;
+    if (a.rank <= 16) lora_down_kernel<DT, 1, TM, 1><<<down, kDownThreads, 0, hs>>>(a);
+    else if (a.rank <= 32) lora_down_kernel<DT, 2, TM, 1><<<down, kDownThreads, 0, hs>>>(a);
+    else if (a.rank <= 64) lora_down_kernel<DT, 4, TM, 1><<<down, kDownThreads, 0, hs>>>(a);
+    else lora_down_kernel<DT, 8, TM / RW, RW><<<down, kDownThreads, 0, hs>>>(a);
     if (a.rank == 8 || a.rank == 16) lora_up_kernel<DT, 0, TM><<<up, kThreads, 0, hs>>>(a);
     else if (a.rank <= 32) lora_up_kernel<DT, 1, TM><<<up, kThreads, 0, hs>>>(a);
     else if (a.rank <= 64) lora_up_kernel<DT, 2, TM><<<up, kThreads, 0, hs>>>(a);
