@@ -127,9 +127,9 @@ def _heads(what, name, x, types, ref=None):
 
 def _strides(x):
     """Strides of tokens and heads; 0 where there is no second one to reach."""
+    t, h, _ = x.stride()
     T, H, _ = x.shape
-    s = x.stride()
-    return s[0] if T > 1 else 0, s[1] if H > 1 else 0
+    return t if T > 1 else 0, h if H > 1 else 0
 
 
 def rotary(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, factor: float = 1.0,
@@ -155,16 +155,18 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, factor
     xs = _strides(x)
     if out is None:
         out = x.new_empty((T, H, D)) if stream is None else _new(stream, x, (T, H, D), x.dtype)
+        os = H * D if T > 1 else 0, D if H > 1 else 0
     else:
         _heads(what, "out", out, {x.dtype: dtype}, x)
         if out.shape != x.shape:
             _fail(_q.QUICK_ERR_INVALID_ARG, "%s: out must have shape %s, not %s", what, tuple(x.shape), tuple(out.shape))
-        if (T > 1 and out.stride(0) < D) or (H > 1 and out.stride(1) < D):
+        os = _strides(out)
+        if (T > 1 and os[0] < D) or (H > 1 and os[1] < D):
             _fail(_q.QUICK_ERR_SHAPE, "%s: rows of out overlap", what)
-        if out.data_ptr() == x.data_ptr() and _strides(out) != xs and x.numel():
+        if out.data_ptr() == x.data_ptr() and os != xs and x.numel():
             _fail(_q.QUICK_ERR_INVALID_ARG, "%s: out must be x with x's strides, or apart from it", what)
     _run(x, "quick_rotary", x.data_ptr(), dtype, *xs, T, H, D, positions.data_ptr(), freqs.data_ptr(), R,
-         int(bool(interleaved)), int(bool(inverse)), factor, out.data_ptr(), *_strides(out), _q._stream(stream, x))
+         int(bool(interleaved)), int(bool(inverse)), factor, out.data_ptr(), *os, _q._stream(stream, x))
     return out
 
 

@@ -12,6 +12,7 @@ module.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -64,8 +65,27 @@ def _rows(what, name, t, ref, T, n):
     return ld
 
 
+@functools.lru_cache(maxsize=256)
 def lora_workspace_bytes(R: int, K: int, E: int, rank: int) -> int:
     return int(_q.lib().quick_lora_workspace_bytes(R, K, E, rank))
+
+
+def _usual(x, y, a, b, offsets, rows, scales):
+    """Whether the checks have nothing to say against a call of contiguous
+    tensors (a small call is bound by the host; one by one they take 3 us)."""
+    if not (x.is_cuda and y.is_cuda and a.is_cuda and b.is_cuda and offsets.is_cuda and rows.is_cuda):
+        return False
+    dev, dtype, i32 = x.get_device(), x.dtype, torch.int32
+    if not (y.get_device() == a.get_device() == b.get_device() == offsets.get_device() == rows.get_device() == dev
+            and y.dtype is dtype and a.dtype is dtype and b.dtype is dtype and offsets.dtype is i32 and rows.dtype is i32
+            and x.is_contiguous() and y.is_contiguous() and a.is_contiguous() and b.is_contiguous()
+            and offsets.is_contiguous() and rows.is_contiguous()):
+        return False
+    if not (x.dim() == y.dim() == 2 and a.dim() == b.dim() == 3 and offsets.dim() == rows.dim() == 1):
+        return False
+    (T, K), (E, rank, k), (e, N, r) = x.shape, a.shape, b.shape
+    return (k == K and e == E and r == rank and y.shape == (T, N) and offsets.shape[0] == E + 1 and rows.shape[0] <= T
+            and (scales is None or (_plain(scales, dev, torch.float32) and scales.shape == (E,))))
 
 
 def lora_add(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor,
@@ -79,24 +99,26 @@ def lora_add(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
     what = "lora_add"
     _gpu(what, "x", x)
     code = _type(what, "x", x.dtype, _TYPES16)
-    if x.dim() != 2 or not isinstance(y, torch.Tensor) or y.dim() != 2:
-        _fail(_q.QUICK_ERR_INVALID_ARG, "%s: x and y must be [T][K] and [T][N]", what)
-    (T, K), N = x.shape, y.shape[1]
-    ldx, ldy = _rows(what, "x", x, x, T, K), _rows(what, "y", y, x, T, N)
-    if not isinstance(a, torch.Tensor) or a.dim() != 3:
-        _fail(_q.QUICK_ERR_INVALID_ARG, "%s: a must be [E][rank][K]", what)
-    E, rank = a.shape[:2]
-    dev = x.get_device()
-    if not (_plain(a, dev, x.dtype) and _plain(b, dev, x.dtype) and a.shape == (E, rank, K) and b.shape == (E, N, rank)):
+    if all(type(t) is torch.Tensor for t in (y, a, b, offsets, rows)) and _usual(x, y, a, b, offsets, rows, scales):
+        (T, K), (E, N, rank), R = x.shape, b.shape, rows.shape[0]
+        ldx, ldy = K, N
+    else:
+        if x.dim() != 2 or not isinstance(y, torch.Tensor) or y.dim() != 2:
+            _fail(_q.QUICK_ERR_INVALID_ARG, "%s: x and y must be [T][K] and [T][N]", what)
+        (T, K), N = x.shape, y.shape[1]
+        ldx, ldy = _rows(what, "x", x, x, T, K), _rows(what, "y", y, x, T, N)
+        if not isinstance(a, torch.Tensor) or a.dim() != 3:
+            _fail(_q.QUICK_ERR_INVALID_ARG, "%s: a must be [E][rank][K]", what)
+        E, rank = a.shape[:2]
         _q._dev(what, "a", a, x, dtype=x.dtype, shape=(E, rank, K))
         _q._dev(what, "b", b, x, dtype=x.dtype, shape=(E, N, rank))
-    if scales is not None:
-        _q._dev(what, "scales", scales, x, dtype=torch.float32, shape=(E,))
-    _int32(what, "offsets", offsets, x, (E + 1,))
-    if not isinstance(rows, torch.Tensor) or rows.dim() != 1 or rows.shape[0] > T:
-        _fail(_q.QUICK_ERR_INVALID_ARG, "%s: rows must be an int32 vector of the tokens", what)
-    R = rows.shape[0]
-    _int32(what, "rows", rows, x, (R,))
+        if scales is not None:
+            _q._dev(what, "scales", scales, x, dtype=torch.float32, shape=(E,))
+        _int32(what, "offsets", offsets, x, (E + 1,))
+        if not isinstance(rows, torch.Tensor) or rows.dim() != 1 or rows.shape[0] > T:
+            _fail(_q.QUICK_ERR_INVALID_ARG, "%s: rows must be an int32 vector of the tokens", what)
+        R = rows.shape[0]
+        _int32(what, "rows", rows, x, (R,))
     if out is None:
         out = x.new_empty((T, N)) if stream is None else _new(stream, x, (T, N), x.dtype)
         ldo = N
