@@ -49,10 +49,11 @@ struct Element<QUICK_F32> {
 };
 
 // A workgroup turns some heads of one token: it works the token's R / 2 pairs
-// of cosine and sine out once, in LDS, and a thread keeps its place in the
-// heads.  The angle is a binary64 product, cut to its turns there (position
-// 2^31 at frequency 1 is then off by 2^-22 of a radian at most), and the rest,
-// at most half a turn, is binary32.
+// of cosine and sine out once, in LDS, while its first loads are under way, and
+// a thread keeps its place in the heads, four of them at a time.  The angle is a
+// binary64 product, cut to its turns there (position 2^31 at frequency 1 is then
+// off by 2^-22 of a radian at most), and the rest, at most half a turn, is
+// binary32.
 // Bound by the bytes, x once and out once; a few tokens by latency.
 template <int DT, int V, bool INTER>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
@@ -62,9 +63,33 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
     struct alignas(sizeof(T) * V) Vec {
         T v[V];
     };
+    constexpr int BATCH = 4;
     __shared__ float2 turn[kMaxChannels / 2];
     const int64_t t = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts;
+    const int wide = min(a.pieces, kThreads);
+    const int first = threadIdx.x % wide, row = threadIdx.x / wide;
+    const int h1 = min(a.H, (part + 1) * a.heads), h0 = row < a.together ? part * a.heads + row : h1;
+    // channels of piece p: of a pair's two places, or of those that stay (once)
+    auto places = [&](int p, int& c, int& d) {
+        if (p >= a.turning) c = d = 2 * a.half + (p - a.turning) * V;
+        else if (INTER) c = p * 2 * V, d = c + V;
+        else c = p * V, d = c + a.half;
+    };
+    Vec u[BATCH], w[BATCH];
+    auto load = [&](int p, int h) {
+        int c, d;
+        places(p, c, d);
+        if (p >= a.turning && !a.copy) return;
+#pragma unroll
+        for (int i = 0; i < BATCH; i++) {
+            if (h + i * a.together >= h1) continue;
+            const T* x = (const T*)a.x + t * a.x_token + (h + i * a.together) * a.x_head;
+            u[i] = *(const Vec*)(x + c);
+            if (p < a.turning) w[i] = *(const Vec*)(x + d);
+        }
+    };
+    load(first, h0);
     for (int i = threadIdx.x; i < a.half; i += kThreads) {
         double r = (double)a.positions[t] * a.freqs[i] * 0.15915494309189533577;   // 1 / (2 pi)
         r -= rint(r);
@@ -73,55 +98,42 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
         turn[i] = make_float2(c * a.factor, s * a.factor * a.sign);
     }
     __syncthreads();
-    const int wide = min(a.pieces, kThreads);
-    const int first = threadIdx.x % wide, row = threadIdx.x / wide;
-    if (row >= a.together) return;
-    const int h0 = part * a.heads, h1 = min(a.H, h0 + a.heads);
     for (int p = first; p < a.pieces; p += wide) {
-        if (p < a.turning) {
-            // channels at c and at d: pairs by place, or side by side
-            const int c = INTER ? p * 2 * V : p * V, d = INTER ? c + V : c + a.half;
-            for (int h = h0 + row; h < h1; h += a.together) {
-                const T* x = (const T*)a.x + t * a.x_token + h * a.x_head;
-                T* o = (T*)a.out + t * a.out_token + h * a.out_head;
-                const Vec u = *(const Vec*)(x + c), w = *(const Vec*)(x + d);
+        int c, d;
+        places(p, c, d);
+        for (int h = h0; h < h1; h += BATCH * a.together) {
+            if (p != first || h != h0) load(p, h);
+#pragma unroll
+            for (int b = 0; b < BATCH; b++) {
+                if (h + b * a.together >= h1) continue;
+                T* o = (T*)a.out + t * a.out_token + (h + b * a.together) * a.out_head;
+                if (p >= a.turning) {
+                    if (a.copy) *(Vec*)(o + c) = u[b];
+                    continue;
+                }
+                T in[2 * V], res[2 * V];
+#pragma unroll
+                for (int i = 0; i < V; i++) {
+                    in[i] = u[b].v[i];
+                    in[V + i] = w[b].v[i];
+                }
+#pragma unroll
+                for (int i = 0; i < V; i++) {
+                    const float2 cs = turn[p * V + i];
+                    const int m = INTER ? 2 * i : i, n = INTER ? 2 * i + 1 : V + i;
+                    const float x = E::get(in[m]), y = E::get(in[n]);
+                    res[m] = E::put(x * cs.x - y * cs.y);
+                    res[n] = E::put(y * cs.x + x * cs.y);
+                }
                 Vec y, z;
-                if constexpr (!INTER) {
 #pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        const float2 cs = turn[p * V + i];
-                        const float m = E::get(u.v[i]), n = E::get(w.v[i]);
-                        y.v[i] = E::put(m * cs.x - n * cs.y);
-                        z.v[i] = E::put(n * cs.x + m * cs.y);
-                    }
-                } else {
-                    T in[2 * V], res[2 * V];
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        in[i] = u.v[i];
-                        in[V + i] = w.v[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        const float2 cs = turn[p * V + i];
-                        const float m = E::get(in[2 * i]), n = E::get(in[2 * i + 1]);
-                        res[2 * i] = E::put(m * cs.x - n * cs.y);
-                        res[2 * i + 1] = E::put(n * cs.x + m * cs.y);
-                    }
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        y.v[i] = res[i];
-                        z.v[i] = res[V + i];
-                    }
+                for (int i = 0; i < V; i++) {
+                    y.v[i] = res[i];
+                    z.v[i] = res[V + i];
                 }
                 *(Vec*)(o + c) = y;
                 *(Vec*)(o + d) = z;
             }
-        } else if (a.copy) {
-            const int c = 2 * a.half + (p - a.turning) * V;
-            for (int h = h0 + row; h < h1; h += a.together)
-                *(Vec*)((T*)a.out + t * a.out_token + h * a.out_head + c) =
-                    *(const Vec*)((const T*)a.x + t * a.x_token + h * a.x_head + c);
         }
     }
 }
@@ -161,12 +173,13 @@ __global__ __launch_bounds__(kThreads) void kv4_write_kernel(CacheArgs a)
     constexpr int P = D / 8, TOKENS = kThreads / P;
     const int h = blockIdx.x % a.heads, p = threadIdx.x % P;
     const int64_t t = (int64_t)(blockIdx.x / a.heads) * TOKENS + threadIdx.x / P;
-    const int64_t slot = t < a.T ? a.slots[t] : -1;
     // the lanes of a block share a token, so they stay together
-    if (slot < 0 || slot >= a.slots_end) return;
+    if (t >= a.T) return;
     u4_t raw[2];
-    raw[0] = *(const u4_t*)(a.k + 2 * (t * a.k_token + h * a.k_head + p * 8));
-    raw[1] = *(const u4_t*)(a.v + 2 * (t * a.v_token + h * a.v_head + p * 8));
+    raw[0] = __builtin_nontemporal_load((const u4_t*)(a.k + 2 * (t * a.k_token + h * a.k_head + p * 8)));
+    raw[1] = __builtin_nontemporal_load((const u4_t*)(a.v + 2 * (t * a.v_token + h * a.v_head + p * 8)));
+    const int64_t slot = a.slots[t];
+    if (slot < 0 || slot >= a.slots_end) return;
     uint8_t* page = a.cache + ((slot / kPage) * a.heads + h) * L::kBytes;
     const int s = (int)(slot % kPage);
 #pragma unroll
