@@ -242,8 +242,8 @@ __device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&
     }
 }
 
-// A few queries of each sequence (16 NC columns at most, a column being a query
-// and one of the heads that share keys and values).  A wave takes every WAVES'th page
+// A few queries of each sequence (tiles of 16 NC columns, a column being a query
+// and one of the heads that share keys and values; NC = 1: one tile each).  A wave takes every WAVES'th page
 // of its workgroup's share: scores transposed, keys . queries^T, so that a
 // column's scores are in the lanes that need its weights as the operand of
 // values^T . weights, with no exchange between lanes and nothing in LDS; the
@@ -264,10 +264,10 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
         walk.h = worker - walk.b * a.s.heads;
         walk.j = walk.at = 0;
         walk.left = walk.share = INT32_MAX;
-    } else walk = find_share<BC, false>(a.s, a.workers, worker, kStreamShare);
+    } else walk = find_share<BC, NC == 2>(a.s, a.workers, worker, kStreamShare);
     int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
-        const Tile t = tile_of<BC>(a.s, walk.b, 0);
+        const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
         const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
         if (left_to_next(a.s, walk, t, take)) break;
         int p0, p1;
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
         Seen seen[NC];
 #pragma unroll
         for (int n = 0; n < NC; n++) {
-            const int cc = n * 16 + c, i = cc * a.group_inv >> 16;
+            const int cc = walk.j * BC + n * 16 + c, i = cc * a.group_inv >> 16;
             const bool live = cc < t.columns;
             const int pos = t.base + i;
             seen[n].hi = !live ? INT32_MAX : a.s.causal ? min(pos + 1, t.length) : t.length;
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
             __syncthreads();
             constexpr int PIECES = D / 8;
             for (int at = threadIdx.x; at < 16 * PIECES; at += 64 * WAVES) {
-                const int x = at / PIECES, d = at % PIECES * 8, cc = n * 16 + x;
+                const int x = at / PIECES, d = at % PIECES * 8, cc = walk.j * BC + n * 16 + x;
                 if (cc >= t.columns) continue;
                 float m = refs[0][x][0];
 #pragma unroll
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
             }
         }
         if (a.whole) return;
-        advance<BC, false>(a.s, walk, t, take);
+        advance<BC, NC == 2>(a.s, walk, t, take);
     }
     if (threadIdx.x < 8) {
         int v = join[0];
@@ -446,16 +446,26 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
     if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
 }
 
-// Columns of a workgroup's tile.
+// Columns of a workgroup's tile, by the most columns n of a sequence (queries
+// and the heads that share keys and values).
+// Up to 128 the stream kernel, in tiles of 32 (16 sequences of 2000 to 8000
+// tokens, 8 cache heads of 128: n = 40 44 us, 64 45, 96 57, 128 71; the tiled
+// one, half of whose waves the first of these leave idle, 59, 62, 67, 73; of 256
+// channels n = 80 127 and 183).  Of the tiled forms 256 columns with many
+// queries: 3 to 5 % faster there (8192 queries of 8 heads each: 1132 us, 1190
+// with 128), and as much slower with few (1 to 501 of 4 heads: 88 us, 83 with
+// 128); its registers do not suffice for 256 channels.
 int columns_of(const quick_attention_t& a)
 {
     const int64_t n = a.most * (a.q_heads / a.heads);
-    return n <= 16 ? 16 : n <= 32 ? 32 : n <= 128 || a.D > 128 ? 128 : 256;
+    if (n <= 128) return n <= 16 ? 16 : 32;
+    return n < 2048 || a.D > 128 ? 128 : 256;
 }
 
-// Whether a workgroup takes an item each: few queries of sequences of 16 pages
-// at most, for which a second launch costs more than unequal lengths do.
-bool whole_items(const quick_attention_t& a) { return columns_of(a) <= 32 && a.table_width <= 16; }
+// Whether a workgroup takes an item each: one tile of a sequence, of 16 pages at
+// most, for which a second launch costs more than unequal lengths do (one
+// sequence of 1000 tokens: 9.9 us, 13.8 shared out).
+bool whole_items(const quick_attention_t& a) { return a.most * (a.q_heads / a.heads) <= 32 && a.table_width <= 16; }
 
 int workers_of(const quick_attention_t& a)
 {

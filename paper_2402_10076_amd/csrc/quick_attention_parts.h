@@ -31,7 +31,7 @@ struct AttnArgs {
     int32_t* joins;       // [workers][8] the item that a worker leaves unfinished
     int64_t q_token, q_head;
     int32_t pages, workers;
-    int32_t group_inv;    // c / group == c * group_inv >> 16 for c < 32
+    int32_t group_inv;    // c / group == c * group_inv >> 16 for c < 128
     int32_t whole;        // a worker takes an item and no more; nothing to join
     float scale;          // of the scores times log2(e), without its sign
     uint32_t q_sign;      // changes q's sign where the scale is negative
