@@ -446,6 +446,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
     if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
 }
 
+// Most columns of a sequence.
+int64_t columns_most(const quick_attention_t& a) { return std::min(a.most, a.T) * (a.q_heads / a.heads); }
+
 // Columns of a workgroup's tile, by the most columns n of a sequence (queries
 // and the heads that share keys and values).
 // Up to 128 the stream kernel, in tiles of 32 (16 sequences of 2000 to 8000
@@ -457,7 +460,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 // 128); its registers do not suffice for 256 channels.
 int columns_of(const quick_attention_t& a)
 {
-    const int64_t n = a.most * (a.q_heads / a.heads);
+    const int64_t n = columns_most(a);
     if (n <= 128) return n <= 16 ? 16 : 32;
     return n < 2048 || a.D > 128 ? 128 : 256;
 }
@@ -465,7 +468,7 @@ int columns_of(const quick_attention_t& a)
 // Whether a workgroup takes an item each: one tile of a sequence, of 16 pages at
 // most, for which a second launch costs more than unequal lengths do (one
 // sequence of 1000 tokens: 9.9 us, 13.8 shared out).
-bool whole_items(const quick_attention_t& a) { return a.most * (a.q_heads / a.heads) <= 32 && a.table_width <= 16; }
+bool whole_items(const quick_attention_t& a) { return columns_most(a) <= 32 && a.table_width <= 16; }
 
 int workers_of(const quick_attention_t& a)
 {
@@ -563,7 +566,7 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
     a.s.seqs = (int32_t)p->seqs;
     a.s.width = (int32_t)p->table_width;
     a.s.most = (int32_t)std::min<int64_t>(p->most, p->T);
-    a.s.window = (int32_t)std::min<int64_t>(p->window, INT32_MAX);
+    a.s.window = (int32_t)std::min<int64_t>(p->window, 1 << 30);   // (tokens are fewer)
     a.s.causal = p->causal != 0;
     a.s.start = columns > 32 ? kTiledStart : kStreamStart;
     a.q = (const uint8_t*)q;

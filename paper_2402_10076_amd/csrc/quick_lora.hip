@@ -108,6 +108,7 @@ struct LoraArgs {
     float* low;           // [slices][R][rank] x . A^T over a slice of the channels
     int64_t ldx, ldy, ldo;
     int32_t T, K, N, E, rank, R, slices, slice;   // slice: channels of one
+    int32_t parts;        // workgroups of a tile in the second product
 };
 
 template <int DT>
@@ -276,7 +277,7 @@ template <int DT, int RS, int TM>
 __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
 {
     constexpr int STEPS = RS ? RS : 1;      // of 32 ranks (RS == 0: rank 8 or 16)
-    const RowTile t = find_tile<16 * TM>(a, blockIdx.y);
+    const RowTile t = find_tile<16 * TM>(a, blockIdx.x / a.parts);
     if (t.count == 0) return;
     const bool bare = t.e == a.E;
     if (bare && a.out == a.y) return;
@@ -343,8 +344,8 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
 #pragma unroll
             for (int h = 0; h < 2; h++) y[m][h] = *(const u4_t*)(ys[m] + 2 * min(n0 + h * 32 + g * 8, a.N - 8));
     };
-    const int step = gridDim.x * 256;
-    int n0 = (blockIdx.x * 4 + wave) * 64;
+    const int step = a.parts * 256;
+    int n0 = ((int)(blockIdx.x % a.parts) * 4 + wave) * 64;
     load_b(n0);
     load_y(n0);
     for (; n0 < a.N; n0 += step) {
@@ -412,14 +413,15 @@ void slices_of(int64_t R, int64_t K, int64_t E, int32_t* slices, int32_t* slice)
 }
 
 template <int DT, int TM>
-void launch_lora(const LoraArgs& a, hipStream_t hs)
+void launch_lora(LoraArgs a, hipStream_t hs)
 {
     const uint32_t tiles = (uint32_t)tiles_of(a.R, a.E);
     // columns: enough workgroups for the chip, and no more, as each begins with the sums over the slices; those of one
     // eighth follow each other eight apart, on one die, whose cache then holds their part of B (15360 columns of rank
     // 64 of four adapters: 42 us, 86 with the tiles on the dies)
     const int64_t most = ceil_div(a.N, 256), want = ceil_div(ceil_div(512, tiles), 8) * 8;
-    const dim3 down(tiles, a.slices), up((uint32_t)std::min(most, want), tiles);
+    a.parts = (int32_t)std::min(most, want);
+    const dim3 down(tiles, a.slices), up(tiles * a.parts);
     // (LDS does not hold the sums of 128 ranks of 64 rows by eight waves)
     constexpr int RW = TM > 1 ? 2 : 1;
     if (a.rank <= 16) lora_down_kernel<DT, 1, TM, 1><<<down, kDownThreads, 0, hs>>>(a);
