@@ -277,19 +277,15 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
         Seen seen[NC];
 #pragma unroll
         for (int n = 0; n < NC; n++) {
-            const int cc = walk.j * BC + n * 16 + c, i = cc * a.group_inv >> 16;
-            const bool live = cc < t.columns;
+            // (columns behind the last are that one again, and go nowhere)
+            const int cc = min(walk.j * BC + n * 16 + c, t.columns - 1), i = cc * a.group_inv >> 16;
             const int pos = t.base + i;
-            seen[n].hi = !live ? INT32_MAX : a.s.causal ? min(pos + 1, t.length) : t.length;
-            seen[n].lo = a.s.window && live ? max(0, pos + 1 - a.s.window) : 0;
+            seen[n].hi = a.s.causal ? min(pos + 1, t.length) : t.length;
+            seen[n].lo = a.s.window ? max(0, pos + 1 - a.s.window) : 0;
             const uint8_t* from = a.q + 2 * ((int64_t)(t.first + i) * a.q_token +
                                              (int64_t)(walk.h * a.s.group + cc - i * a.s.group) * a.q_head);
 #pragma unroll
-            for (int j = 0; j < KW; j++) {
-                const int piece = D == 64 ? 2 * g + j : 16 * (j / 4) + 4 * g + j % 4;
-                q[n][j] = u4_t{0, 0, 0, 0};
-                if (live) q[n][j] = *(const u4_t*)(from + piece * 16) ^ a.q_sign;
-            }
+            for (int j = 0; j < KW; j++) q[n][j] = *(const u4_t*)(from + (D == 64 ? 2 * g + j : 16 * (j / 4) + 4 * g + j % 4) * 16);
             col[n].m = kNothing;
             col[n].l = 0;
 #pragma unroll
@@ -312,6 +308,13 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
             page = page_of(0, ok);
             load_keys<D>(keys, page, lane);
             load_values<D>(values, page, lane);
+        }
+        if (a.q_sign) {
+            seldom();
+#pragma unroll
+            for (int n = 0; n < NC; n++)
+#pragma unroll
+                for (int j = 0; j < KW; j++) q[n][j] ^= a.q_sign;
         }
         for (int n = 0; n < count; n++) {
             const int token0 = (p0 + wave + WAVES * n) * kPage;

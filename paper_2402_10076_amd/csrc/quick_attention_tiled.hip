@@ -188,20 +188,18 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
         if (left_to_next(a.s, walk, t, take)) break;
         int p0, p1;
         pages_of(a.s, t, walk.at, take, p0, p1);
-        const int cc = walk.j * BC + wave * 32 + (lane & 31), i = cc / a.s.group;
-        const bool live = cc < t.columns, work = walk.j * BC + wave * 32 < t.columns;
+        // (columns behind the last are that one again, and go nowhere)
+        const int place = walk.j * BC + wave * 32 + (lane & 31), cc = min(place, t.columns - 1), i = cc / a.s.group;
+        const bool live = place < t.columns, work = walk.j * BC + wave * 32 < t.columns;
         const int pos = t.base + i;
-        const int hi = !live ? INT32_MAX : a.s.causal ? min(pos + 1, t.length) : t.length;
-        const int lo = a.s.window && live ? max(0, pos + 1 - a.s.window) : 0;
+        const int hi = a.s.causal ? min(pos + 1, t.length) : t.length;
+        const int lo = a.s.window ? max(0, pos + 1 - a.s.window) : 0;
         const int64_t head = (int64_t)walk.h * a.s.group + cc - i * a.s.group;
         u4_t q[KS];
         {
-            const uint8_t* from = a.q + 2 * ((int64_t)(t.first + i) * a.q_token + head * a.q_head);
+            const uint8_t* from = a.q + 2 * ((int64_t)(t.first + i) * a.q_token + head * a.q_head) + half * 16;
 #pragma unroll
-            for (int s = 0; s < KS; s++) {
-                q[s] = u4_t{0, 0, 0, 0};
-                if (live) q[s] = *(const u4_t*)(from + (2 * s + half) * 16) ^ a.q_sign;
-            }
+            for (int s = 0; s < KS; s++) q[s] = *(const u4_t*)(from + s * 32);
         }
         float m = kNothing, l = 0;
         f16_t o[VT];
@@ -303,6 +301,11 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
         if (count) {
             id = table[p0];
             fetch(0);
+            if (a.q_sign) {
+                seldom();
+#pragma unroll
+                for (int s = 0; s < KS; s++) q[s] ^= a.q_sign;
+            }
             Unstage<DT, D, NW> un;
             un.template step<0>(next, tiles[0], wave, lane);
             un.template step<1>(next, tiles[0], wave, lane);
