@@ -167,14 +167,12 @@ __device__ __forceinline__ void weigh(f4_t (&s)[NC][4], Column<D> (&col)[NC], co
     for (int n = 0; n < NC; n++) {
         if (masked) {
             seldom();
-            const int lo = seen[n].lo - token0, hi = ok ? seen[n].hi - token0 : 0;
+            const int lo = seen[n].lo - token0 - 4 * g, hi = (ok ? seen[n].hi : token0) - token0 - 4 * g;
+            const uint32_t bits[2] = {bits_between(lo, hi), bits_between(lo - 32, hi - 32)};
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int t = 16 * i + 4 * g + e;
-                    s[n][i][e] = t >= lo && t < hi ? s[n][i][e] : -INFINITY;
-                }
+                for (int e = 0; e < 4; e++) s[n][i][e] = where_bit(s[n][i][e], bits[i / 2], 16 * (i % 2) + e);
         }
         float top = s[n][0][0];
 #pragma unroll
@@ -292,12 +290,14 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
             for (int j = 0; j < D / 16; j++) col[n].o[j] = f4_t{0, 0, 0, 0};
         }
         const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
+        const uint8_t* head = a.cache + walk.h * L::kBytes;
+        const uint32_t stride = a.s.heads * L::kBytes;
         int32_t ids = 0;
         auto page_of = [&](int n, bool& inside) {    // page n of this wave
             if ((n & 63) == 0) ids = table[min(p0 + wave + WAVES * (n + lane), p1 - 1)];
             const int x = __builtin_amdgcn_readlane(ids, n & 63);
             inside = x >= 0 && x < a.pages;
-            return a.cache + ((int64_t)(inside ? x : 0) * a.s.heads + walk.h) * L::kBytes;
+            return head + (int64_t)(inside ? x : 0) * stride;
         };
         const int count = p1 > p0 + wave ? (p1 - p0 - wave + WAVES - 1) / WAVES : 0;
         KeyWords<D> keys;

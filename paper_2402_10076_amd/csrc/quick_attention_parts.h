@@ -73,10 +73,21 @@ __device__ __forceinline__ uint32_t pair16(float a, float b)
 // Keeps a seldom taken branch a branch: the compiler would rather work both
 // sides out and select.
 __device__ __forceinline__ void seldom() { asm volatile("" ::); }
-// The scale that byte i of a word of scales stands for.
-__device__ __forceinline__ float scale_of(uint32_t w, int i)
+// The scale that byte i of a word of scales stands for, for code_pair: its byte is
+// the exponent.  The conversion reads nothing else of a scale (tried with every
+// code, exponent and 64 patterns of the other bits), so those hold what comes.
+__device__ __forceinline__ float scale_of(uint32_t w, int i) { return bits_as<float>(i == 3 ? w >> 1 : w << (23 - 8 * i)); }
+// Bits lo <= i < hi of a word, any lo and hi.
+__device__ __forceinline__ uint32_t bits_between(int lo, int hi)
 {
-    return bits_as<float>(i == 3 ? w >> 1 & 0x7F800000u : (i == 2 ? w << 7 : i == 1 ? w << 15 : w << 23) & 0x7F800000u);
+    const uint32_t below = hi >= 32 ? ~0u : hi <= 0 ? 0u : (1u << hi) - 1;
+    return below & (lo >= 32 ? 0u : lo <= 0 ? ~0u : ~0u << lo);
+}
+// v where bit i of a word is set, else minus infinity.
+__device__ __forceinline__ float where_bit(float v, uint32_t bits, int i)
+{
+    const uint32_t m = (uint32_t)((int32_t)(bits << (31 - i)) >> 31);
+    return bits_as<float>((bits_as<uint32_t>(v) & m) | (0xFF800000u & ~m));
 }
 template <int DT>
 __device__ __forceinline__ f4_t mfma16(u4_t a, u4_t b, f4_t c)

@@ -98,7 +98,7 @@ struct Unstage {
 #pragma unroll
         for (int h = 0; h < S::HALVES; h++) {
             if constexpr (STEP == 0) {
-                const float scale = bits_as<float>((s.ks[h] >> (8 * w) & 255u) << 23);
+                const float scale = bits_as<float>(__builtin_amdgcn_alignbit(s.ks[h], s.ks[h], 8 * w + 9));     // (byte w)
 #pragma unroll
                 for (int j = 0; j < S::KW; j++) {
                     // word n of a lane: channels 8 n .. of its 32 (D == 64: 16)
@@ -109,9 +109,12 @@ struct Unstage {
             if constexpr (STEP == 1) {
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    const uint32_t b = beyond<DT>(s.vs[h][i]);
-                    mark |= b;
-                    s.vs[h][i] &= ~((b >> 7) * 0xFFu);
+                    mark |= beyond<DT>(s.vs[h][i]);
+                }
+                if (__ballot(mark != 0)) {
+                    seldom();
+#pragma unroll
+                    for (int i = 0; i < 2; i++) s.vs[h][i] &= ~((beyond<DT>(s.vs[h][i]) >> 7) * 0xFFu);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
@@ -208,6 +211,8 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
 #pragma unroll
             for (int r = 0; r < 16; r++) o[j][r] = 0;
         const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
+        const uint8_t* head_of_cache = a.cache + walk.h * L::kBytes;
+        const uint32_t stride = a.s.heads * L::kBytes;
         const int count = max(0, p1 - p0);
         Staged<D, NW> next;
         const uint8_t* next_page = a.cache;
@@ -218,7 +223,7 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             const int x = (int)uniform((uint32_t)id);
             id = table[min(p0 + n + 1, p1 - 1)];
             next_ok = x >= 0 && x < a.pages;
-            next_page = a.cache + ((int64_t)(next_ok ? x : 0) * a.s.heads + walk.h) * L::kBytes;
+            next_page = head_of_cache + (int64_t)(next_ok ? x : 0) * stride;
             stage<D, NW>(next, next_page, wave, lane);
         };
         // scores of half x of a page
@@ -232,12 +237,10 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
         auto refer = [&](f16_t& s, int token0, bool ok) {
             if (token0 + 32 > t.all_hi || token0 < t.all_lo || !ok) {
                 seldom();
-                const int to = ok ? hi : INT32_MIN;
+                const int from = token0 + 4 * half;
+                const uint32_t bits = bits_between(lo - from, (ok ? hi : from) - from);
 #pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    const int token = token0 + r / 4 * 8 + 4 * half + r % 4;
-                    s[r] = token >= lo && token < to ? s[r] : -INFINITY;
-                }
+                for (int r = 0; r < 16; r++) s[r] = where_bit(s[r], bits, r / 4 * 8 + r % 4);
             }
             float top = s[0];
 #pragma unroll
