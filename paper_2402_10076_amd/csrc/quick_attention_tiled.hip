@@ -422,7 +422,7 @@ void launch(const AttnArgs& a, int columns, hipStream_t hs)
     if constexpr (D <= 128) {
         if (columns == 256) return attn_tiled_kernel<DT, D, 8, 3><<<a.workers, 512, 0, hs>>>(a);
     }
-    attn_tiled_kernel<DT, D, 4, 2><<<a.workers, 256, 0, hs>>>(a);
+    attn_tiled_kernel<DT, D, 4, D == 64 ? 3 : 2><<<a.workers, 256, 0, hs>>>(a);
 }
 template <int DT>
 void launch(const AttnArgs& a, int64_t D, int columns, hipStream_t hs)
