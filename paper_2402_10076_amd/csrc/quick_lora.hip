@@ -265,6 +265,18 @@ __global__ __launch_bounds__(kDownThreads) void lora_down_kernel(LoraArgs a)
     }
 }
 
+// Swaps b of the lanes c < 8 of each 16 with a of the lanes c + 8.
+__device__ __forceinline__ void swap_eights(u4_t& a, u4_t& b, bool low)
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t x = low ? b[i] : a[i];
+        const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, false);    // (row_ror:8)
+        a[i] = low ? a[i] : y;
+        b[i] = low ? y : b[i];
+    }
+}
+
 // out = y + low . B^T of a tile of 16 TM rows, 64 columns a wave at a time.  The
 // rows of B are the instruction's rows, in an order that leaves a lane twice 8
 // consecutive columns of its token, and four lanes 64 bytes: row 4 g + i of tile
@@ -283,14 +295,15 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
     if (bare && a.out == a.y) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
     // (what is behind the rows, the columns or the rank is read from another place and goes nowhere)
-    int row[TM];
-    const uint8_t* ys[TM];
+    const bool front = c < 8;
+    int row[TM][2];
 #pragma unroll
-    for (int m = 0; m < TM; m++) {
-        const int at = m * 16 + c, x = a.rows[t.first + min(at, t.count - 1)];
-        row[m] = at < t.count && x >= 0 && x < a.T ? x : -1;
-        ys[m] = a.y + 2 * ((int64_t)max(row[m], 0) * a.ldy);
-    }
+    for (int m = 0; m < TM; m++)
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int at = m * 16 + 8 * k + (c & 7), x = a.rows[t.first + min(at, t.count - 1)];
+            row[m][k] = at < t.count && x >= 0 && x < a.T ? x : -1;
+        }
     // with a low rank every lane group holds the same of it (8 g % rank)
     const int per = RS ? 1 : 32 / a.rank, mine = RS ? 0 : g * 8 / a.rank;
     u4_t low[STEPS][TM];
@@ -338,11 +351,14 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
                 if (RS && s == STEPS - 1 && r >= a.rank) w[s][j] = u4_t{0, 0, 0, 0};
             }
     };
+    // a load has 128 bytes of eight rows: of lanes c and c + 8 the two halves of the row (c & 7) or (c & 7) + 8
+    const int column = (c >> 3) * 32 + g * 8;
     auto load_y = [&](int n0) {
 #pragma unroll
         for (int m = 0; m < TM; m++)
 #pragma unroll
-            for (int h = 0; h < 2; h++) y[m][h] = *(const u4_t*)(ys[m] + 2 * min(n0 + h * 32 + g * 8, a.N - 8));
+            for (int k = 0; k < 2; k++)
+                y[m][k] = *(const u4_t*)(a.y + 2 * ((int64_t)max(row[m][k], 0) * a.ldy + min(n0 + column, a.N - 8)));
     };
     const int step = a.parts * 256;
     int n0 = ((int)(blockIdx.x % a.parts) * 4 + wave) * 64;
@@ -375,20 +391,24 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
         // the next columns' operands take the place of these as they are done with
         load_b(n0 + step);
 #pragma unroll
-        for (int m = 0; m < TM; m++)
+        for (int m = 0; m < TM; m++) {
+            if (!bare) {
+                swap_eights(y[m][0], y[m][1], front);
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int n = n0 + h * 32 + g * 8;
-                if (row[m] < 0 || n >= a.N) continue;
-                u4_t o;
+                for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const f4_t v = acc[m][h * 2 + i / 2];
-                    o[i] = to16x2<DT>(from16<DT>((uint16_t)y[m][h][i]) + v[i % 2 * 2],
-                                      from16<DT>((uint16_t)(y[m][h][i] >> 16)) + v[i % 2 * 2 + 1]);
-                }
-                *(u4_t*)(a.out + 2 * ((int64_t)row[m] * a.ldo + n)) = bare ? y[m][h] : o;
+                    for (int i = 0; i < 4; i++) {
+                        const f4_t v = acc[m][h * 2 + i / 2];
+                        y[m][h][i] = to16x2<DT>(from16<DT>((uint16_t)y[m][h][i]) + v[i % 2 * 2],
+                                                from16<DT>((uint16_t)(y[m][h][i] >> 16)) + v[i % 2 * 2 + 1]);
+                    }
+                swap_eights(y[m][0], y[m][1], front);
             }
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+                if (row[m][k] >= 0 && n0 + column < a.N)
+                    *(u4_t*)(a.out + 2 * ((int64_t)row[m][k] * a.ldo + n0 + column)) = y[m][k];
+        }
         load_y(n0 + step);
     }
 }
