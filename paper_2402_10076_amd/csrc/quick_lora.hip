@@ -346,9 +346,15 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
                 // with a low rank load j is that of tiles per * j .. per * j + per - 1
                 if (per * j >= 4) continue;
                 const int tile = RS ? j : per * j + mine, r = RS ? s * 32 + g * 8 : g * 8 % a.rank;
-                const int n = min(n0 + (tile >> 1) * 32 + (c >> 2) * 8 + (tile & 1) * 4 + (c & 3), a.N - 1);
-                w[s][j] = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + min(r, a.rank - 8)));
-                if (RS && s == STEPS - 1 && r >= a.rank) w[s][j] = u4_t{0, 0, 0, 0};
+                if constexpr (RS > 1) {
+                    // (of a pair of steps in the order of y's lines)
+                    const int x = s % 2 * 8 + (c & 7), n = min(n0 + (tile >> 1) * 32 + (x >> 2) * 8 + (tile & 1) * 4 + (x & 3), a.N - 1);
+                    w[s][j] = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + min(s / 2 * 64 + (c >> 3) * 32 + g * 8, a.rank - 8)));
+                } else {
+                    const int n = min(n0 + (tile >> 1) * 32 + (c >> 2) * 8 + (tile & 1) * 4 + (c & 3), a.N - 1);
+                    w[s][j] = *(const u4_t*)(b + 2 * ((int64_t)n * a.rank + min(r, a.rank - 8)));
+                    if (RS && s == STEPS - 1 && r >= a.rank) w[s][j] = u4_t{0, 0, 0, 0};
+                }
             }
     };
     // a load has 128 bytes of eight rows: of lanes c and c + 8 the two halves of the row (c & 7) or (c & 7) + 8
@@ -381,6 +387,13 @@ __global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
                     acc[m][j] = mfma16<DT>(here ? v : u4_t{0, 0, 0, 0}, here ? low[0][m] : u4_t{0, 0, 0, 0}, acc[m][j]);
             }
         } else {
+#pragma unroll
+            for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    if (RS > 1 && s % 2 == 0) swap_eights(w[s][j], w[s + 1][j], front);
+                    if (RS > 1 && s * 32 + g * 8 >= a.rank) w[s][j] = u4_t{0, 0, 0, 0};
+                }
 #pragma unroll
             for (int s = 0; s < STEPS; s++)
 #pragma unroll
