@@ -286,7 +286,7 @@ __device__ __forceinline__ void swap_eights(u4_t& a, u4_t& b, bool low)
 // for that group's lanes, so that every load is full.
 // Bound by the bytes of y and out for many rows.
 template <int DT, int RS, int TM>
-__global__ __launch_bounds__(kThreads, 2) void lora_up_kernel(LoraArgs a)
+__global__ __launch_bounds__(kThreads, RS == 4 && TM == 4 ? 1 : 2) void lora_up_kernel(LoraArgs a)
 {
     constexpr int STEPS = RS ? RS : 1;      // of 32 ranks (RS == 0: rank 8 or 16)
     const RowTile t = find_tile<16 * TM>(a, blockIdx.x / a.parts);
