@@ -280,8 +280,8 @@ __device__ __forceinline__ void swap_eights(u4_t& a, u4_t& b, bool low)
 // out = y + low . B^T of a tile of 16 TM rows, 64 columns a wave at a time.  The
 // rows of B are the instruction's rows, in an order that leaves a lane twice 8
 // consecutive columns of its token, and four lanes 64 bytes: row 4 g + i of tile
-// j is column 32 (j / 2) + 8 g + 4 (j % 2) + i.  The sums of low over the slices, scaled and rounded, are the other operand
-// and stay in registers for all columns.  With a rank of 8 or 16 a lane group's
+// j is column 32 (j / 2) + 8 g + 4 (j % 2) + i.  The sums of low over the slices,
+// scaled and rounded, are the other operand and stay in registers for all columns.  With a rank of 8 or 16 a lane group's
 // 16 bytes of B are of another tile (or of two), and both operands are zero but
 // for that group's lanes, so that every load is full.
 // Bound by the bytes of y and out for many rows.
@@ -307,31 +307,30 @@ __global__ __launch_bounds__(kThreads, RS == 4 && TM == 4 ? 1 : 2) void lora_up_
     // with a low rank every lane group holds the same of it (8 g % rank)
     const int per = RS ? 1 : 32 / a.rank, mine = RS ? 0 : g * 8 / a.rank;
     u4_t low[STEPS][TM];
-    const float scale = !bare && a.scales ? a.scales[t.e] : 1.0f;
     if (!bare) {
-        f4_t u[STEPS][TM], v[STEPS][TM];
-#pragma unroll
-        for (int s = 0; s < STEPS; s++)
-#pragma unroll
-            for (int m = 0; m < TM; m++) u[s][m] = v[s][m] = f4_t{0, 0, 0, 0};
-        // all of a slice's loads are under way together
-        for (int n = 0; n < a.slices; n++) {
-#pragma unroll
-            for (int s = 0; s < STEPS; s++)
-#pragma unroll
-                for (int m = 0; m < TM; m++) {
-                    const int r = RS ? min(s * 32 + g * 8, a.rank - 8) : g * 8 % a.rank;
-                    const float* from = a.low + ((int64_t)n * a.R + t.first + min(m * 16 + c, t.count - 1)) * a.rank + r;
-                    u[s][m] += *(const f4_t*)from;
-                    v[s][m] += *(const f4_t*)(from + 4);
-                }
+        // the sums over the slices once a workgroup
+        __shared__ u4_t lows[16 * TM][4 * STEPS + 1];
+        const float scale = a.scales ? a.scales[t.e] : 1.0f;
+        const int pieces = a.rank / 8;
+        for (int i = threadIdx.x; i < 16 * TM * pieces; i += kThreads) {
+            const int x = i / pieces, r = i - x * pieces;
+            const float* from = a.low + ((int64_t)t.first + min(x, t.count - 1)) * a.rank + r * 8;
+            f4_t u{0, 0, 0, 0}, v{0, 0, 0, 0};
+#pragma unroll 4
+            for (int n = 0; n < a.slices; n++) {
+                u += *(const f4_t*)(from + (int64_t)n * a.R * a.rank);
+                v += *(const f4_t*)(from + (int64_t)n * a.R * a.rank + 4);
+            }
+            u *= scale;
+            v *= scale;
+            lows[x][r] = u4_t{to16x2<DT>(u[0], u[1]), to16x2<DT>(u[2], u[3]), to16x2<DT>(v[0], v[1]), to16x2<DT>(v[2], v[3])};
         }
+        __syncthreads();
 #pragma unroll
         for (int s = 0; s < STEPS; s++)
 #pragma unroll
             for (int m = 0; m < TM; m++) {
-                const f4_t p = u[s][m] * scale, q = v[s][m] * scale;
-                low[s][m] = u4_t{to16x2<DT>(p[0], p[1]), to16x2<DT>(p[2], p[3]), to16x2<DT>(q[0], q[1]), to16x2<DT>(q[2], q[3])};
+                low[s][m] = lows[m * 16 + c][RS ? s * 4 + g : g % pieces];
                 if (RS && s * 32 + g * 8 >= a.rank) low[s][m] = u4_t{0, 0, 0, 0};
             }
     }
