@@ -481,7 +481,7 @@ int workers_of(const quick_attention_t& a)
     const int64_t rows = std::min(a.T, a.seqs * std::min(a.most, a.T));
     const int64_t items = (std::min(a.seqs, a.T) + rows * group / bc + 1) * a.heads;
     const int64_t least = bc > 32 ? kTiledShare : kStreamShare;
-    const int64_t most = bc == 256 ? kTiledWorkers8 : bc == 128 ? kTiledWorkers4 : kUnits * stream_resident(a.D, (int)bc / 16);
+    const int64_t most = bc > 32 ? tiled_workers(a.D, bc) : kUnits * stream_resident(a.D, (int)bc / 16);
     const int64_t shares = std::max<int64_t>(1, (a.table_width + least - 1) / least);
     return (int)(items > most / shares ? most : items * shares);
 }

@@ -141,9 +141,12 @@ __device__ __forceinline__ void value_words(const uint32_t (&a)[W], const uint32
     }
 }
 
-// The tiled kernel: workgroups of four waves (128 columns) and of eight (256),
-// least share, and what an item costs beside its pages.
-constexpr int kTiledWorkers4 = 512, kTiledWorkers8 = 256, kTiledShare = 10, kTiledStart = 6;
+// The tiled kernel: workgroups that the chip holds (two a compute unit, one of 256
+// columns or of 256 channels, whose registers leave a wave a SIMD; 2 x 2048
+// queries of 4 heads of 256: 505 us, 530 with twice as many), least share, and
+// what an item costs beside its pages.
+constexpr int tiled_workers(int64_t D, int64_t columns) { return D > 128 || columns > 128 ? 256 : 512; }
+constexpr int kTiledShare = 10, kTiledStart = 6;
 void launch_tiled_attention(const AttnArgs& a, int dtype, int64_t D, int columns, hipStream_t hs);
 
 }  // namespace quick
