@@ -178,7 +178,7 @@ __device__ __forceinline__ RowTile find_tile(const LoraArgs& a, int index)
 
 // low = x . A^T of a tile of 16 TM RW rows and a slice of the channels.  Of eight
 // waves RW share the rows out, 16 TM each, and the others the channels, each
-// taking 128 at a time; the rows of A (16 RT of them) are the instruction's
+// taking 128 (64 of many rows) at a time; the rows of A (16 RT of them) are the instruction's
 // rows, those of x its columns, both straight from memory, 16 bytes a lane; the
 // waves' sums meet in LDS.  A tile is a chain of latencies: offsets, rows,
 // operands, LDS.
@@ -186,7 +186,7 @@ template <int DT, int RT, int TM, int RW>
 __global__ __launch_bounds__(kDownThreads) void lora_down_kernel(LoraArgs a)
 {
     constexpr int KW = kDownThreads / 64 / RW, ROWS = 16 * TM * RW;
-    constexpr int STEPS = RT * TM > 8 ? 2 : 4;     // of 32 channels whose operands are loaded together
+    constexpr int STEPS = TM > 1 ? 2 : 4, TAKE = 32 * STEPS;    // of 32 channels whose operands are loaded together
     __shared__ float sums[KW][ROWS][16 * RT + 4];
     const RowTile t = find_tile<ROWS>(a, blockIdx.x);
     if (t.count == 0 || t.e == a.E) return;
@@ -210,43 +210,40 @@ __global__ __launch_bounds__(kDownThreads) void lora_down_kernel(LoraArgs a)
 #pragma unroll
         for (int r = 0; r < RT; r++) acc[m][r] = f4_t{0, 0, 0, 0};
     if (row0 < t.count) {
-        for (int k = k0 + part * 128; k < k1; k += KW * 128) {
+        for (int k = k0 + part * TAKE; k < k1; k += KW * TAKE) {
+            u4_t xv[STEPS][TM], wv[STEPS][RT];
+            if (k + TAKE <= k1) {
 #pragma unroll
-            for (int s0 = 0; s0 < 4; s0 += STEPS) {
-                u4_t xv[STEPS][TM], wv[STEPS][RT];
-                if (k + 128 <= k1) {
+                for (int s = 0; s < STEPS; s++) {
 #pragma unroll
-                    for (int s = 0; s < STEPS; s++) {
+                    for (int m = 0; m < TM; m++) xv[s][m] = *(const u4_t*)(x[m] + 2 * (k + s * 32));
 #pragma unroll
-                        for (int m = 0; m < TM; m++) xv[s][m] = *(const u4_t*)(x[m] + 2 * (k + (s0 + s) * 32));
+                    for (int r = 0; r < RT; r++) wv[s][r] = *(const u4_t*)(w[r] + 2 * (k + s * 32));
+                }
+            } else {
+                // the last channels: eights behind the end are zero in both
 #pragma unroll
-                        for (int r = 0; r < RT; r++) wv[s][r] = *(const u4_t*)(w[r] + 2 * (k + (s0 + s) * 32));
+                for (int s = 0; s < STEPS; s++) {
+                    const bool in = k + s * 32 + g * 8 < k1;
+                    const int64_t at = in ? k + s * 32 : k0 - g * 8;
+#pragma unroll
+                    for (int m = 0; m < TM; m++) {
+                        const u4_t v = *(const u4_t*)(x[m] + 2 * at);
+                        xv[s][m] = in ? v : u4_t{0, 0, 0, 0};
                     }
-                } else {
-                    // the last channels: eights behind the end are zero in both
 #pragma unroll
-                    for (int s = 0; s < STEPS; s++) {
-                        const bool in = k + (s0 + s) * 32 + g * 8 < k1;
-                        const int64_t at = in ? k + (s0 + s) * 32 : k0 - g * 8;
-#pragma unroll
-                        for (int m = 0; m < TM; m++) {
-                            const u4_t v = *(const u4_t*)(x[m] + 2 * at);
-                            xv[s][m] = in ? v : u4_t{0, 0, 0, 0};
-                        }
-#pragma unroll
-                        for (int r = 0; r < RT; r++) {
-                            const u4_t v = *(const u4_t*)(w[r] + 2 * at);
-                            wv[s][r] = in ? v : u4_t{0, 0, 0, 0};
-                        }
+                    for (int r = 0; r < RT; r++) {
+                        const u4_t v = *(const u4_t*)(w[r] + 2 * at);
+                        wv[s][r] = in ? v : u4_t{0, 0, 0, 0};
                     }
                 }
-#pragma unroll
-                for (int s = 0; s < STEPS; s++)
-#pragma unroll
-                    for (int m = 0; m < TM; m++)
-#pragma unroll
-                        for (int r = 0; r < RT; r++) acc[m][r] = mfma16<DT>(wv[s][r], xv[s][m], acc[m][r]);
             }
+#pragma unroll
+            for (int s = 0; s < STEPS; s++)
+#pragma unroll
+                for (int m = 0; m < TM; m++)
+#pragma unroll
+                    for (int r = 0; r < RT; r++) acc[m][r] = mfma16<DT>(wv[s][r], xv[s][m], acc[m][r]);
         }
 #pragma unroll
         for (int m = 0; m < TM; m++)
@@ -436,11 +433,13 @@ int64_t tiles_of(int64_t R, int64_t E)
 }
 
 // Slices of the channels: a workgroup for each compute unit and some more, whole
-// rounds of its waves (1024 channels).
+// rounds of its waves (64 channels each with 64 rows, 128 with 16), and eight at
+// most, as the second product adds them up.
 void slices_of(int64_t R, int64_t K, int64_t E, int32_t* slices, int32_t* slice)
 {
-    const int64_t rounds = ceil_div(K, 1024), n = std::max<int64_t>(1, std::min(rounds, 320 / tiles_of(R, E)));
-    *slice = (int32_t)(ceil_div(rounds, n) * 1024);
+    const int64_t round = tile_rows(R, E) == 64 ? 512 : 1024, rounds = ceil_div(K, round);
+    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, 8), 320 / tiles_of(R, E)));
+    *slice = (int32_t)(ceil_div(rounds, n) * round);
     *slices = (int32_t)ceil_div(K, *slice);
 }
 
