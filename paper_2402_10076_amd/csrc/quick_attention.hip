@@ -246,6 +246,10 @@ __device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&
 // column's scores are in the lanes that need its weights as the operand of
 // values^T . weights, with no exchange between lanes and nothing in LDS; the
 // waves' sums meet in LDS once an item.
+// Long sequences are bound by HBM: 64 of 512 to 32768 tokens, 8 heads of 128 read
+// by 8 each, 207 us, 5.6 TB/s; short shares by the chain of plan, table, page and
+// the sums' meeting, some 15 thousand cycles an item: 32 sequences of 37 to 4096,
+// 32 heads, 52 us, 5.5 TB/s; 8 of 2000 to 9000, 5 queries, 21 us, 2.3 TB/s.
 template <int DT, int D, int NC, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_stream_kernel(AttnArgs a)
 {
@@ -413,7 +417,8 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
 // Joins the parts of the item that a worker left unfinished: its own, and the
 // first ones of the workers after it.  A thread has eight channels of a column;
 // the parts' references first, so that the loads of their sums are independent
-// of each other.
+// of each other.  A launch and a chain of three loads: 4.6 us (decode), 15 (8192
+// queries of 64 heads, 29 MB).
 template <int DT, int D, int BC>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
@@ -455,12 +460,12 @@ int64_t columns_most(const quick_attention_t& a) { return std::min(a.most, a.T) 
 // Columns of a workgroup's tile, by the most columns n of a sequence (queries
 // and the heads that share keys and values).
 // Up to 128 the stream kernel, in tiles of 32 (16 sequences of 2000 to 8000
-// tokens, 8 cache heads of 128: n = 40 44 us, 64 45, 96 57, 128 71; the tiled
-// one, half of whose waves the first of these leave idle, 59, 62, 67, 73; of 256
-// channels n = 80 127 and 183).  Of the tiled forms 256 columns with many
-// queries: 3 to 5 % faster there (8192 queries of 8 heads each: 1132 us, 1190
-// with 128), and as much slower with few (1 to 501 of 4 heads: 88 us, 83 with
-// 128); its registers do not suffice for 256 channels.
+// tokens, 8 cache heads of 128: n = 40 43 us, 64 44, 96 57, 128 71; the tiled
+// one, half of whose waves the first of these leave idle, 57, 60, 65, 72; of 256
+// channels n = 80 124 and 162).  Of the tiled forms 256 columns with many
+// queries: 7 % faster there (8192 queries of 8 heads each: 1109 us, 1194 with
+// 128), and as much slower with few (1 to 501 of 4 heads of 64, a window: 84 us,
+// 76 with 128); its registers do not suffice for 256 channels.
 int columns_of(const quick_attention_t& a)
 {
     const int64_t n = columns_most(a);
@@ -470,7 +475,7 @@ int columns_of(const quick_attention_t& a)
 
 // Whether a workgroup takes an item each: one tile of a sequence, of 16 pages at
 // most, for which a second launch costs more than unequal lengths do (one
-// sequence of 1000 tokens: 9.9 us, 13.8 shared out).
+// sequence of 1000 tokens: 9.8 us, 13.9 shared out).
 bool whole_items(const quick_attention_t& a) { return columns_most(a) <= 32 && a.table_width <= 16; }
 
 int workers_of(const quick_attention_t& a)

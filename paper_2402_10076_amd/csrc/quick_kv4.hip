@@ -54,7 +54,8 @@ struct Element<QUICK_F32> {
 // binary64 product, cut to its turns there (position 2^31 at frequency 1 is then
 // off by 2^-22 of a radian at most), and the rest, at most half a turn, is
 // binary32.
-// Bound by the bytes, x once and out once; a few tokens by latency.
+// Bound by the bytes, x once and out once: 8192 tokens of 72 heads of 128 (64
+// turned) take 54.6 us, 5.5 TB/s; a few tokens by latency (2.8 us).
 template <int DT, int V, bool INTER>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
 {
@@ -165,7 +166,9 @@ struct CacheArgs {
 // neighbouring lanes a block, as in quick_mxfp4_quantize.  Tokens that follow
 // each other share the 128-byte lines of the values' order, and one workgroup
 // writes them.
-// Bound by the bytes: 2 in, 17/32 out per value; a few tokens by the launch.
+// Bound by the bytes: 2 in, 17/32 out per value; a few tokens by the launch (3
+// us).  8192 tokens of 32 heads of 128: 33 us, 5.1 TB/s, with slots in order; 42
+// with slots in random order, whose parts of lines make twice the bytes written.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void kv4_write_kernel(CacheArgs a)
 {
@@ -212,7 +215,7 @@ __device__ __forceinline__ float code_value(uint32_t n, float k)
     return bits_as<float>(bits_as<uint32_t>(m) | (n & 8u) << 28) * k;
 }
 
-// The same threads the other way.
+// The same threads the other way (those 8192 tokens: 32.5 us, 5.2 TB/s).
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void kv4_read_kernel(CacheArgs a)
 {

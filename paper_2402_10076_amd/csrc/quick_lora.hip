@@ -180,8 +180,9 @@ __device__ __forceinline__ RowTile find_tile(const LoraArgs& a, int index)
 // waves RW share the rows out, 16 TM each, and the others the channels, each
 // taking 128 (64 of many rows) at a time; the rows of A (16 RT of them) are the instruction's
 // rows, those of x its columns, both straight from memory, 16 bytes a lane; the
-// waves' sums meet in LDS.  A tile is a chain of latencies: offsets, rows,
-// operands, LDS.
+// waves' sums meet in LDS.
+// A tile is a chain of latencies: offsets, rows, operands, LDS (4096 tokens of
+// 5120 channels, rank 64: 20 us, 7 by its bytes).
 template <int DT, int RT, int TM, int RW>
 __global__ __launch_bounds__(kDownThreads) void lora_down_kernel(LoraArgs a)
 {
@@ -281,7 +282,12 @@ __device__ __forceinline__ void swap_eights(u4_t& a, u4_t& b, bool low)
 // scaled and rounded, are the other operand and stay in registers for all columns.  With a rank of 8 or 16 a lane group's
 // 16 bytes of B are of another tile (or of two), and both operands are zero but
 // for that group's lanes, so that every load is full.
-// Bound by the bytes of y and out for many rows.
+// A lane's loads and stores of y, and its loads of B, are of the two halves of
+// eight rows' 128 bytes, put in the product's order by an exchange of lanes
+// eight apart: two loads of 64 bytes of a line wait for each other (4096 tokens,
+// 15360 columns of rank 64: 99.6 us with the first product, 90.4 so).
+// Bound by the bytes of y and out for many rows: there 64 us, 3.9 TB/s, of 44 at
+// the rate of a copy; the rest is B, 126 MB through L2, and the start of a tile.
 template <int DT, int RS, int TM>
 __global__ __launch_bounds__(kThreads, RS == 4 && TM == 4 ? 1 : 2) void lora_up_kernel(LoraArgs a)
 {
@@ -433,12 +439,13 @@ int64_t tiles_of(int64_t R, int64_t E)
 }
 
 // Slices of the channels: a workgroup for each compute unit and some more, whole
-// rounds of its waves (64 channels each with 64 rows, 128 with 16), and eight at
-// most, as the second product adds them up.
+// rounds of its waves (64 channels each with 64 rows, 128 with 16), and 16 at
+// most, as the second product adds them up (512 tokens, 5120 channels: 27.2 us,
+// 29.2 with eight).
 void slices_of(int64_t R, int64_t K, int64_t E, int32_t* slices, int32_t* slice)
 {
     const int64_t round = tile_rows(R, E) == 64 ? 512 : 1024, rounds = ceil_div(K, round);
-    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, 8), 320 / tiles_of(R, E)));
+    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, 16), 320 / tiles_of(R, E)));
     *slice = (int32_t)(ceil_div(rounds, n) * round);
     *slices = (int32_t)ceil_div(K, *slice);
 }
@@ -449,7 +456,7 @@ void launch_lora(LoraArgs a, hipStream_t hs)
     const uint32_t tiles = (uint32_t)tiles_of(a.R, a.E);
     // columns: enough workgroups for the chip, and no more, as each begins with the sums over the slices; those of one
     // eighth follow each other eight apart, on one die, whose cache then holds their part of B (15360 columns of rank
-    // 64 of four adapters: 42 us, 86 with the tiles on the dies)
+    // 64 of four adapters, 1024 tokens: 31.5 us, 36.8 with the tiles on the dies; 4096: the same within 1 %)
     const int64_t most = ceil_div(a.N, 256), want = ceil_div(ceil_div(512, tiles), 8) * 8;
     a.parts = (int32_t)std::min(most, want);
     const dim3 down(tiles, a.slices), up(tiles * a.parts);
