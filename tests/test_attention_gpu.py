@@ -257,3 +257,14 @@ def test_nothing_to_do():
     q = torch.ones((2, 4, 64), dtype=torch.float16, device="cuda")
     two = torch.tensor([5, 0], dtype=torch.int32, device="cuda")
     assert not Q.kv4_attention(q, cache, torch.zeros((2, 0), dtype=torch.int32, device="cuda"), two).any()
+
+
+@pytest.mark.parametrize("width", [None, 40], ids=["short", "long"])
+@pytest.mark.parametrize("group,most", [(1, 4), (4, 4), (8, 4), (8, 40), (40, 4)])
+@pytest.mark.parametrize("new", [[0, 3, 0, 1], [0, 0, 2, 0], [1, 0, 0, 0], [0, 0, 0, 4]], ids=lambda v: "".join(map(str, v)))
+def test_sequences_without_a_query(new, group, most, width):
+    """Such sequences have no columns: nothing of the queries before the first or behind the last is read or written."""
+    say("without a query", new, group, most, width)
+    b = Batch(31, [70, 9, 300, 5], new, 2, group, 128, "f16", width=width)
+    b.check(most=most)
+    b.check(most=most, causal=False)
