@@ -261,8 +261,9 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
     const int worker = blockIdx.x;
     Walk walk;
     if (a.whole) {
-        // an item each: no joining
+        // an item each: no joining, and no place for it
         walk.b = worker / a.s.heads;
+        if (seq_of(a.s, walk.b).queries == 0) return;
         walk.h = worker - walk.b * a.s.heads;
         walk.j = walk.at = 0;
         walk.left = walk.share = INT32_MAX;
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
         const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
         const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
-        if (t.columns == 0 || left_to_next(a.s, walk, t, take)) break;     // (a whole item's sequence may have no query)
+        if (left_to_next(a.s, walk, t, take)) break;
         int p0, p1;
         pages_of(a.s, t, walk.at, take, p0, p1);
         u4_t q[NC][KW];
