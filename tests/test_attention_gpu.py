@@ -268,3 +268,13 @@ def test_sequences_without_a_query(new, group, most, width):
     b = Batch(31, [70, 9, 300, 5], new, 2, group, 128, "f16", width=width)
     b.check(most=most)
     b.check(most=most, causal=False)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("window", [2, 31, 32, 33, 60, 63, 64, 65, 68, 95, 96, 97, 128])
+def test_window_edges(window, new, D):
+    """Windows that begin and end at every kind of place in a half page, a page and a lane's tokens."""
+    say("window edges", window, new, D)
+    b = Batch(32, [200, 193, 161], [new] * 3, 1, 4, D, "f16")
+    b.check(window=window)

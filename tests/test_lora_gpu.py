@@ -136,3 +136,12 @@ def test_nothing_to_do():
     a, b = torch.zeros((2, 8, 64), dtype=torch.float16, device="cuda"), torch.zeros((2, 64, 8), dtype=torch.float16, device="cuda")
     o, r = Q.lora_group(torch.empty(0, dtype=torch.int32, device="cuda"), 2)
     assert not o.any() and Q.lora_add(e, e, a, b, o, r).shape == (0, 64)
+
+
+@pytest.mark.parametrize("T,K,N,E,r", [(400, 2600, 1096, 3, 72), (512, 5128, 328, 2, 64), (192, 9000, 72, 1, 8), (49, 9000, 136, 1, 120)])
+def test_many_slices(T, K, N, E, r):
+    """Many channels for few tiles: slices of them that the second product adds up, the last one short."""
+    x, y, a, b, ids, scales = _case(9, T, K, N, E, r, "bf16")
+    say("slices", T, K, N, E, r)
+    out = Q.lora_add(y.cuda(), x.cuda(), a.cuda(), b.cuda(), *Q.lora_group(ids.cuda(), E), scales=scales.cuda())
+    _check(out, x, y, a, b, ids, scales)
