@@ -250,7 +250,7 @@ __device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&
 // by 8 each, 207 us, 5.6 TB/s; short shares by the chain of plan, table, page and
 // the sums' meeting, some 15 thousand cycles an item: 32 sequences of 37 to 4096,
 // 32 heads, 52 us, 5.5 TB/s; 8 of 2000 to 9000, 5 queries, 21 us, 2.3 TB/s.
-template <int DT, int D, int NC, int WAVES>
+template <int DT, int D, int NC, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_stream_kernel(AttnArgs a)
 {
     typedef Kv4<D> L;
@@ -260,51 +260,68 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int worker = blockIdx.x;
     Walk walk;
-    if (a.whole) {
-        // an item each: no joining, and no place for it
+    int32_t ids = 0;
+    if constexpr (WHOLE) {
+        // an item each: no joining, and no place for it; all of a sequence's pages come while its length does
         walk.b = worker / a.s.heads;
-        if (seq_of(a.s, walk.b).queries == 0) return;
         walk.h = worker - walk.b * a.s.heads;
         walk.j = walk.at = 0;
         walk.left = walk.share = INT32_MAX;
+        if (a.s.width) ids = a.table[(int64_t)walk.b * a.s.width + min(lane, a.s.width - 1)];
     } else walk = find_share<BC, NC == 2>(a.s, a.workers, worker, kStreamShare);
     int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
-        const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
+        const Seq seq = seq_of(a.s, walk.b);
+        const int columns = seq.queries * a.s.group;
+        if (WHOLE && columns == 0) return;
+        // (columns behind the last are that one again, and go nowhere)
+        u4_t q[NC][KW];
+        int of[NC];
+        auto load_queries = [&] {
+#pragma unroll
+            for (int n = 0; n < NC; n++) {
+                const int cc = min(walk.j * BC + n * 16 + c, columns - 1);
+                of[n] = cc * a.group_inv >> 16;
+                const uint8_t* from = a.q + 2 * ((int64_t)(seq.first + of[n]) * a.q_token +
+                                                 (int64_t)(walk.h * a.s.group + cc - of[n] * a.s.group) * a.q_head);
+#pragma unroll
+                for (int j = 0; j < KW; j++)
+                    q[n][j] = *(const u4_t*)(from + (D == 64 ? 2 * g + j : 16 * (j / 4) + 4 * g + j % 4) * 16);
+            }
+        };
+        if (WHOLE) load_queries();      // (they need no length)
+        const Tile t = tile_of<BC>(a.s, seq, walk.j);
         const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
-        if (left_to_next(a.s, walk, t, take)) break;
+        if (!WHOLE && left_to_next(a.s, walk, t, take)) break;
         int p0, p1;
         pages_of(a.s, t, walk.at, take, p0, p1);
-        u4_t q[NC][KW];
+        const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
+        const int count = p1 > p0 + wave ? (p1 - p0 - wave + WAVES - 1) / WAVES : 0;
+        if (!WHOLE) {
+            // the first pages' ids ahead of the queries, for which nothing waits yet
+            if (count) ids = table[min(p0 + wave + WAVES * lane, p1 - 1)];
+            load_queries();
+        }
         Column<D> col[NC];
         Seen seen[NC];
 #pragma unroll
         for (int n = 0; n < NC; n++) {
-            // (columns behind the last are that one again, and go nowhere)
-            const int cc = min(walk.j * BC + n * 16 + c, t.columns - 1), i = cc * a.group_inv >> 16;
-            const int pos = t.base + i;
+            const int pos = t.base + of[n];
             seen[n].hi = a.s.causal ? min(pos + 1, t.length) : t.length;
             seen[n].lo = a.s.window ? max(0, pos + 1 - a.s.window) : 0;
-            const uint8_t* from = a.q + 2 * ((int64_t)(t.first + i) * a.q_token +
-                                             (int64_t)(walk.h * a.s.group + cc - i * a.s.group) * a.q_head);
-#pragma unroll
-            for (int j = 0; j < KW; j++) q[n][j] = *(const u4_t*)(from + (D == 64 ? 2 * g + j : 16 * (j / 4) + 4 * g + j % 4) * 16);
             col[n].m = kNothing;
             col[n].l = 0;
 #pragma unroll
             for (int j = 0; j < D / 16; j++) col[n].o[j] = f4_t{0, 0, 0, 0};
         }
-        const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
         const uint8_t* head = a.cache + walk.h * L::kBytes;
         const uint32_t stride = a.s.heads * L::kBytes;
-        int32_t ids = 0;
         auto page_of = [&](int n, bool& inside) {    // page n of this wave
-            if ((n & 63) == 0) ids = table[min(p0 + wave + WAVES * (n + lane), p1 - 1)];
-            const int x = __builtin_amdgcn_readlane(ids, n & 63);
+            if (!WHOLE && n && (n & 63) == 0) ids = table[min(p0 + wave + WAVES * (n + lane), p1 - 1)];
+            const int x = __builtin_amdgcn_readlane(ids, WHOLE ? p0 + wave + WAVES * n : n & 63);
             inside = x >= 0 && x < a.pages;
             return head + (int64_t)(inside ? x : 0) * stride;
         };
-        const int count = p1 > p0 + wave ? (p1 - p0 - wave + WAVES - 1) / WAVES : 0;
         KeyWords<D> keys;
         ValueWords<D> values;
         bool ok = false;
@@ -404,7 +421,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
                 }
             }
         }
-        if (a.whole) return;
+        if (WHOLE) return;
         advance<BC, NC == 2>(a.s, walk, t, take);
     }
     if (threadIdx.x < 8) {
@@ -498,11 +515,11 @@ void launch_stream(const AttnArgs& a, hipStream_t hs)
     if (a.whole) {
         // few items: more waves each (whose registers do not suffice for 32 columns of 256 channels)
         if constexpr (D * NC < 512) {
-            if (a.workers <= 2 * kUnits) return attn_stream_kernel<DT, D, NC, 8><<<a.workers, 512, 0, hs>>>(a);
+            if (a.workers <= 2 * kUnits) return attn_stream_kernel<DT, D, NC, 8, true><<<a.workers, 512, 0, hs>>>(a);
         }
-        return attn_stream_kernel<DT, D, NC, 4><<<a.workers, 256, 0, hs>>>(a);
+        return attn_stream_kernel<DT, D, NC, 4, true><<<a.workers, 256, 0, hs>>>(a);
     }
-    attn_stream_kernel<DT, D, NC, 4><<<a.workers, 256, 0, hs>>>(a);
+    attn_stream_kernel<DT, D, NC, 4, false><<<a.workers, 256, 0, hs>>>(a);
     attn_join_kernel<DT, D, 16 * NC><<<dim3(a.workers, (2 * NC * D + 255) / 256), 256, 0, hs>>>(a);
 }
 template <int DT, int D>
