@@ -15,6 +15,8 @@ constexpr int stream_resident(int64_t D, int NC) { return D == 64 ? 6 - 2 * NC :
 constexpr int kUnits = 256;
 // What a workgroup takes at least, and what an item costs beside its pages.
 constexpr int kStreamShare = 16, kStreamStart = 12;
+// Most pages of an item that a workgroup takes whole: a wave's lanes hold their ids.
+constexpr int kWholePages = 64;
 
 // Exchanges over the four groups of 16 lanes that share a column.
 template <class F>
@@ -491,10 +493,20 @@ int columns_of(const quick_attention_t& a)
     return n < 2048 || a.D > 128 ? 128 : 256;
 }
 
-// Whether a workgroup takes an item each: one tile of a sequence, of 16 pages at
-// most, for which a second launch costs more than unequal lengths do (one
-// sequence of 1000 tokens: 9.8 us, 13.9 shared out).
-bool whole_items(const quick_attention_t& a) { return columns_most(a) <= 32 && a.table_width <= 16; }
+// Whether a workgroup takes an item each: one tile of a sequence, of so few pages
+// that a second launch, and the plan before the first page, cost more than unequal
+// lengths do.  Of 8 cache heads of 128 read by 4 each, against shared out: 1
+// sequence of 1000 tokens 9.8 us and 13.9, of 3000 12.7 and 13.9, of 4000 15.9 and
+// 14.1; 64 of 1500 21.6 and 23.3, 256 of 100 to 3000 89 and 95.  Many items even
+// out by themselves: 1024 of 37 to 4096 tokens 62.3 and 64.4, though of 8 long
+// sequences among 128 short ones 30 and 24.  32 columns of 256 channels leave a
+// unit four waves: 16 of 100 to 3000 38 and 34.
+bool whole_items(const quick_attention_t& a)
+{
+    const int64_t n = columns_most(a), items = a.seqs * a.heads;
+    if (n > 32) return false;
+    return a.table_width <= (n > 16 && a.D > 128 ? 16 : items < 1024 ? 48 : kWholePages);
+}
 
 int workers_of(const quick_attention_t& a)
 {

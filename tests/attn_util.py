@@ -107,8 +107,12 @@ def attention(q, k, v, lengths, offsets, group, dtype, scale=None, window=0, cau
             out[rows, h] = one
             # weights rounded to the type; they and their sum off by `far`; binary32 sums of n; weights that f16
             # holds below its normal range (2^-25 of a largest of 2^6 or more); the result rounded
+            # (f16: steps of 2^-24 below 2^-14, so that half of one, 2^-25, is the least: a result of 4.0745e-6 became
+            # 68 * 2^-24 = 4.0531e-6, off by 2.14e-8 of 2^-25 = 2.98e-8)
+            least = 2.0 ** -25 if dtype is torch.float16 else 0.0
             tol[rows, h] = (size * (step + 2 * far + n * 2.0 ** -23)
-                            + n * 2.0 ** -31 * vv[:, :].abs().nan_to_num(0).amax() + one.abs() * step + 1e-30)
+                            + n * 2.0 ** -31 * vv[:, :].abs().nan_to_num(0).amax() + (one.abs() * step).clamp(min=least)
+                            + 1e-30)
             lse[rows, h] = torch.where(total > 0, top + torch.log(total), -math.inf).squeeze(1)
     return out, lse, tol
 

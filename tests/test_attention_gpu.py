@@ -259,7 +259,7 @@ def test_nothing_to_do():
     assert not Q.kv4_attention(q, cache, torch.zeros((2, 0), dtype=torch.int32, device="cuda"), two).any()
 
 
-@pytest.mark.parametrize("width", [None, 40], ids=["short", "long"])
+@pytest.mark.parametrize("width", [None, 70], ids=["short", "long"])
 @pytest.mark.parametrize("group,most", [(1, 4), (4, 4), (8, 4), (8, 40), (40, 4)])
 @pytest.mark.parametrize("new", [[0, 3, 0, 1], [0, 0, 2, 0], [1, 0, 0, 0], [0, 0, 0, 4]], ids=lambda v: "".join(map(str, v)))
 def test_sequences_without_a_query(new, group, most, width):
@@ -278,3 +278,39 @@ def test_window_edges(window, new, D):
     say("window edges", window, new, D)
     b = Batch(32, [200, 193, 161], [new] * 3, 1, 4, D, "f16")
     b.check(window=window)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,group,D", [(1, 1, 64), (2, 4, 128), (3, 5, 64), (1, 16, 256), (8, 8, 128), (1, 24, 128), (2, 20, 256)])
+@pytest.mark.parametrize("lengths", LENGTHS + [[2500, 40, 1100]], ids=lambda v: "-".join(map(str, v)))
+def test_wide_tables(lengths, heads, group, D, dtype):
+    """Shares of items, whatever the lengths turn out to be: single tokens and drafts of one, none or two."""
+    say("wide", lengths, heads, group, D, dtype)
+    Batch(33, lengths, [1] * len(lengths), heads, group, D, dtype, width=70).check(offsets=None)
+    b = Batch(34, lengths, [(i + 2) % 3 for i in range(len(lengths))], heads, group, D, dtype, width=70)
+    b.check()
+    b.check(window=70, scale=-0.1)
+    b.check(causal=False)
+
+
+@pytest.mark.parametrize("lengths,heads", [([130, 3000, 64, 0, 1025], 2), ([4000, 77], 2), ([3000] + [65] * 80, 1)], ids=str)
+@pytest.mark.parametrize("D,group,new", [(64, 4, 1), (128, 4, 1), (128, 8, 4), (256, 4, 2)])
+def test_tables_of_middling_width(lengths, heads, D, group, new):
+    """Where items are taken whole, and from where on they are shared out."""
+    say("middling", lengths, heads, D, group, new)
+    for width in (None, 48, 49):
+        if width is None or max(lengths) <= 64 * width:
+            b = Batch(35, lengths, [min(new, max(n, 1)) for n in lengths], heads, group, D, "f16", width=width)
+            b.check()
+            b.check(window=900)
+
+
+def test_many_sequences_shared_and_whole():
+    """More items than are resident: 64 pages each are taken whole, 65 shared out."""
+    g = A.gen(36)
+    lengths = torch.randint(0, 150, (130,), generator=g).tolist() + [64 * 64]
+    for width in (64, 65):
+        Batch(37, lengths, [1] * 131, 8, 1, 64, "bf16", width=width).check(offsets=None)
+    lengths = torch.randint(0, 90, (600,), generator=g).tolist()
+    new = [min(n, int(x)) for n, x in zip(lengths, torch.randint(0, 3, (600,), generator=g))]
+    Batch(38, lengths, new, 1, 2, 64, "f16", width=70).check()

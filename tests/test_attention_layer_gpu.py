@@ -253,5 +253,5 @@ def test_workspaces_that_are_given():
             out = Q.kv4_attention(q[:n], c, table, lengths, offsets=o, most=most, workspace=ws)
             assert torch.equal(out, Q.kv4_attention(q[:n], c, table, lengths, offsets=o, most=most))
     with pytest.raises(Q.QuickError) as e:
-        Q.kv4_attention(q[:2], c, table, lengths, workspace=ws[:64])
+        Q.kv4_attention(q, c, table, lengths, offsets=o, most=200, workspace=ws[:64])
     assert e.value.status == Q.QUICK_ERR_WORKSPACE

@@ -242,7 +242,7 @@ def test_abi_rotary_and_cache():
 
 def test_abi_attention():
     L = Q.lib()
-    base = dict(T=6, q_heads=8, heads=2, D=64, pages=9, seqs=3, table_width=40, most=2, q_token=512, q_head=64, window=0,
+    base = dict(T=6, q_heads=8, heads=2, D=64, pages=9, seqs=3, table_width=100, most=2, q_token=512, q_head=64, window=0,
                 causal=1, scale=1.0)
 
     def struct(**k):
