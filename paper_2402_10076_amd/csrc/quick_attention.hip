@@ -249,9 +249,10 @@ __device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&
 // values^T . weights, with no exchange between lanes and nothing in LDS; the
 // waves' sums meet in LDS once an item.
 // Long sequences are bound by HBM: 64 of 512 to 32768 tokens, 8 heads of 128 read
-// by 8 each, 207 us, 5.6 TB/s; short shares by the chain of plan, table, page and
-// the sums' meeting, some 15 thousand cycles an item: 32 sequences of 37 to 4096,
-// 32 heads, 52 us, 5.5 TB/s; 8 of 2000 to 9000, 5 queries, 21 us, 2.3 TB/s.
+// by 8 each, 207 us, 5.6 TB/s; 32 of 37 to 4096, 32 heads, 62 us, 4.6 TB/s, the
+// longest at the end.  Short shares are bound by the chain of plan, table, page
+// and the sums' meeting, some 15 thousand cycles an item: 8 of 2000 to 9000, 5
+// queries, 21 us, 2.3 TB/s; 1 of 1000, whole, 7 us.
 template <int DT, int D, int NC, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_stream_kernel(AttnArgs a)
 {

@@ -182,7 +182,7 @@ __device__ __forceinline__ RowTile find_tile(const LoraArgs& a, int index)
 // rows, those of x its columns, both straight from memory, 16 bytes a lane; the
 // waves' sums meet in LDS.
 // A tile is a chain of latencies: offsets, rows, operands, LDS (4096 tokens of
-// 5120 channels, rank 64: 20 us, 7 by its bytes).
+// 5120 channels, rank 64: 19 us, 7 by its bytes).
 template <int DT, int RT, int TM, int RW>
 __global__ __launch_bounds__(kDownThreads) void lora_down_kernel(LoraArgs a)
 {
