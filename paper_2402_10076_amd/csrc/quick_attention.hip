@@ -17,6 +17,8 @@ constexpr int kUnits = 256;
 constexpr int kStreamShare = 16, kStreamStart = 12;
 // Most pages of an item that a workgroup takes whole: a wave's lanes hold their ids.
 constexpr int kWholePages = 64;
+// Most sequences that such workgroups put in order.
+constexpr int kRanked = 128;
 
 // Exchanges over the four groups of 16 lanes that share a column.
 template <class F>
@@ -242,6 +244,45 @@ __device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&
     }
 }
 
+// The sequence of rank r, those of the most pages first and equal ones in their
+// order: items beyond the resident ones even out when the longest begin first.
+// Every workgroup counts the sequences by their pages, 64 at most, and looks for
+// its own.  32 sequences of 37 to 4096 tokens, 32 heads: 54.9 us, 62.1 in the order
+// they come in; 128 equal ones of 4000, 8 heads: 106 and 103; many sequences, whose
+// items are short, lose more (1000 of 50 to 500: 104 and 80) and are left alone.
+template <int THREADS>
+__device__ __forceinline__ int of_rank(const AttnShape& s, int r)
+{
+    __shared__ uint32_t count[64];
+    __shared__ uint8_t of[kRanked];
+    const int lane = threadIdx.x & 63;
+    if (threadIdx.x < 64) count[threadIdx.x] = 0;
+    __syncthreads();
+    for (int b = threadIdx.x; b < s.seqs; b += THREADS) {
+        const int from_most = kWholePages - clamped((seq_of(s, b).length + kPage - 1) / kPage, 1, kWholePages);
+        of[b] = (uint8_t)from_most;
+        atomicAdd(&count[from_most], 1u);
+    }
+    __syncthreads();
+    const int n = (int)count[lane];
+    int64_t upto = n;
+    upto = add_from<0x111, 0xF>(upto);
+    upto = add_from<0x112, 0xF>(upto);
+    upto = add_from<0x114, 0xF>(upto);
+    upto = add_from<0x118, 0xF>(upto);
+    upto = add_from<0x142, 0xA>(upto);
+    upto = add_from<0x143, 0xC>(upto);
+    const int at = __builtin_ctzll(__ballot(upto > r));     // (r is less than their sum)
+    int k = r - __builtin_amdgcn_readlane((int)upto - n, at);
+    for (int b0 = 0; b0 < s.seqs; b0 += 64) {
+        const uint64_t m = __ballot(b0 + lane < s.seqs && of[min(b0 + lane, s.seqs - 1)] == at);
+        const int c = __popcll(m);
+        if (k < c) return b0 + __builtin_ctzll(__ballot((m >> lane & 1) && __popcll(m & ((1ull << lane) - 1)) == k));
+        k -= c;
+    }
+    return 0;
+}
+
 // A few queries of each sequence (tiles of 16 NC columns, a column being a query
 // and one of the heads that share keys and values; NC = 1: one tile each).  A wave takes every WAVES'th page
 // of its workgroup's share: scores transposed, keys . queries^T, so that a
@@ -249,10 +290,10 @@ __device__ __forceinline__ void add_values(const ValueWords<D>& w, const u4_t (&
 // values^T . weights, with no exchange between lanes and nothing in LDS; the
 // waves' sums meet in LDS once an item.
 // Long sequences are bound by HBM: 64 of 512 to 32768 tokens, 8 heads of 128 read
-// by 8 each, 207 us, 5.6 TB/s; 32 of 37 to 4096, 32 heads, 62 us, 4.6 TB/s, the
-// longest at the end.  Short shares are bound by the chain of plan, table, page
-// and the sums' meeting, some 15 thousand cycles an item: 8 of 2000 to 9000, 5
-// queries, 21 us, 2.3 TB/s; 1 of 1000, whole, 7 us.
+// by 8 each, 207 us, 5.6 TB/s; 32 of 37 to 4096, 32 heads, 55 us, 5.2 TB/s.  Short
+// shares are bound by the chain of plan, table, page and the sums' meeting, some 15
+// thousand cycles an item: 8 of 2000 to 9000, 5 queries, 21 us, 2.3 TB/s; 1 of
+// 1000, whole, 7 us.
 template <int DT, int D, int NC, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_stream_kernel(AttnArgs a)
 {
@@ -267,7 +308,11 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
     if constexpr (WHOLE) {
         // an item each: no joining, and no place for it; all of a sequence's pages come while its length does
         walk.b = worker / a.s.heads;
-        walk.h = worker - walk.b * a.s.heads;
+        const int rank = walk.b;
+        if constexpr (WAVES == 4) {
+            if (a.ranked) walk.b = of_rank<64 * WAVES>(a.s, rank);
+        }
+        walk.h = worker - rank * a.s.heads;
         walk.j = walk.at = 0;
         walk.left = walk.share = INT32_MAX;
         if (a.s.width) ids = a.table[(int64_t)walk.b * a.s.width + min(lane, a.s.width - 1)];
@@ -499,9 +544,9 @@ int columns_of(const quick_attention_t& a)
 // lengths do.  Of 8 cache heads of 128 read by 4 each, against shared out: 1
 // sequence of 1000 tokens 9.8 us and 13.9, of 3000 12.7 and 13.9, of 4000 15.9 and
 // 14.1; 64 of 1500 21.6 and 23.3, 256 of 100 to 3000 89 and 95.  Many items even
-// out by themselves: 1024 of 37 to 4096 tokens 62.3 and 64.4, though of 8 long
-// sequences among 128 short ones 30 and 24.  32 columns of 256 channels leave a
-// unit four waves: 16 of 100 to 3000 38 and 34.
+// out when the longest begin first: 1024 of 37 to 4096 tokens 54.9 and 64.4; 8
+// sequences of 4091 among 128 of 60 22.3 and 24.4.  32 columns of 256 channels
+// leave a unit four waves: 16 of 100 to 3000 38 and 34.
 bool whole_items(const quick_attention_t& a)
 {
     const int64_t n = columns_most(a), items = a.seqs * a.heads;
@@ -595,6 +640,8 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
     AttnArgs a{};
     a.workers = workers_of(*p);
     a.whole = whole_items(*p);
+    // (fewer items begin at once; more sequences than that even out)
+    a.ranked = a.whole && a.workers > 2 * kUnits && p->seqs > 1 && p->seqs <= kRanked;
     const int columns = columns_of(*p);
     a.s.lengths = lengths;
     a.s.offsets = offsets;

@@ -33,6 +33,7 @@ struct AttnArgs {
     int32_t pages, workers;
     int32_t group_inv;    // c / group == c * group_inv >> 16 for c < 128
     int32_t whole;        // a worker takes an item and no more; nothing to join
+    int32_t ranked;       // ... the longest sequences first
     float scale;          // of the scores times log2(e), without its sign
     uint32_t q_sign;      // changes q's sign where the scale is negative
 };

@@ -314,3 +314,15 @@ def test_many_sequences_shared_and_whole():
     lengths = torch.randint(0, 90, (600,), generator=g).tolist()
     new = [min(n, int(x)) for n, x in zip(lengths, torch.randint(0, 3, (600,), generator=g))]
     Batch(38, lengths, new, 1, 2, 64, "f16", width=70).check()
+
+
+@pytest.mark.parametrize("seqs,heads", [(65, 8), (128, 5), (129, 4), (1030, 1), (3, 300)])
+def test_whole_items_in_any_order(seqs, heads):
+    """More items than begin at once: the longest first, equal ones, empty ones and sequences without a query among
+    them, and more sequences than are put in order."""
+    g = A.gen(39, seqs)
+    lengths = [int(n) * 40 for n in torch.randint(0, 9, (seqs,), generator=g)]
+    new = [int(n) for n in torch.randint(0, 3, (seqs,), generator=g)]
+    say("whole items", seqs, heads)
+    Batch(40, lengths, [min(m, n) for m, n in zip(new, lengths)], heads, 1, 64, "f16").check()
+    Batch(41, [70] * seqs, [1] * seqs, heads, 2, 64, "bf16").check(offsets=None)
