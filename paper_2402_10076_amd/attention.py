@@ -237,6 +237,47 @@ def _attention(*fields):
     return ctypes.byref(a), int(_q.lib().quick_kv4_attention_workspace_bytes(ctypes.byref(a)))
 
 
+def _usual(q, cache, table, lengths, offsets):
+    """Sizes (T, q_heads, pages, heads, D, seqs, width) of a call that the checks
+    have nothing to say against, else None (a small call is bound by the host;
+    one by one they take twice as long)."""
+    if not (type(q) is type(cache) is type(table) is type(lengths) is torch.Tensor):
+        return None
+    dev, i32 = q.get_device(), torch.int32
+    if not (dev == cache.get_device() == table.get_device() == lengths.get_device() and q.is_cuda and q.dim() == 3
+            and cache.dim() == 3 and table.dim() == 2 and q.dtype in _TYPES16 and cache.dtype is torch.uint8
+            and table.dtype is i32 and lengths.dtype is i32 and cache.is_contiguous() and table.is_contiguous()
+            and lengths.is_contiguous() and q.stride(2) == 1):
+        return None
+    (T, HQ, D), (pages, heads, wide), (B, width) = q.shape, cache.shape, table.shape
+    if wide != 68 * D or D not in KV4_DIMS or not heads or HQ % heads or not HQ or lengths.shape != (B,):
+        return None
+    if T != B if offsets is None else not (_plain(offsets, dev, i32) and offsets.shape == (B + 1,)):
+        return None
+    return T, HQ, pages, heads, D, B, width
+
+
+def _checked(q, cache, table, lengths, offsets):
+    """The same sizes, or what is wrong with the call."""
+    what = "kv4_attention"
+    _heads(what, "q", q, _TYPES16)
+    pages, heads, D = _cache(what, cache, q)
+    T, HQ, QD = q.shape
+    if QD != D or HQ % heads or HQ == 0:
+        _fail(_q.QUICK_ERR_SHAPE, "%s: q must be [T][a multiple of %d][%d] for this cache, not %s", what, heads, D,
+              tuple(q.shape))
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        _fail(_q.QUICK_ERR_INVALID_ARG, "%s: table must be an int32 [seqs][width] tensor", what)
+    B, width = table.shape
+    _int32(what, "table", table, q, (B, width))
+    _int32(what, "lengths", lengths, q, (B,))
+    if offsets is not None:
+        _int32(what, "offsets", offsets, q, (B + 1,))
+    elif T != B:
+        _fail(_q.QUICK_ERR_SHAPE, "%s: without offsets q has a row for each of the %d sequences, not %d", what, B, T)
+    return T, HQ, pages, heads, D, B, width
+
+
 def kv4_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                   offsets: torch.Tensor | None = None, most: int | None = None, scale: float | None = None,
                   window: int = 0, causal: bool = True, out: torch.Tensor | None = None,
@@ -259,24 +300,15 @@ def kv4_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, len
     sum.  workspace: a tensor of kv4_attention_workspace_bytes(); one is taken
     from torch's allocator if none is given."""
     what = "kv4_attention"
-    dtype = _heads(what, "q", q, _TYPES16)
-    pages, heads, D = _cache(what, cache, q)
-    T, HQ, QD = q.shape
-    if QD != D or HQ % heads or HQ == 0:
-        _fail(_q.QUICK_ERR_SHAPE, "%s: q must be [T][a multiple of %d][%d] for this cache, not %s", what, heads, D,
-              tuple(q.shape))
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        _fail(_q.QUICK_ERR_INVALID_ARG, "%s: table must be an int32 [seqs][width] tensor", what)
-    B, width = table.shape
-    _int32(what, "table", table, q, (B, width))
-    _int32(what, "lengths", lengths, q, (B,))
-    if offsets is not None:
-        _int32(what, "offsets", offsets, q, (B + 1,))
-        most = max(1, T) if most is None else most
-    else:
-        if T != B:
-            _fail(_q.QUICK_ERR_SHAPE, "%s: without offsets q has a row for each of the %d sequences, not %d", what, B, T)
+    sizes = _usual(q, cache, table, lengths, offsets)
+    if sizes is None:
+        sizes = _checked(q, cache, table, lengths, offsets)
+    T, HQ, pages, heads, D, B, width = sizes
+    dtype = _TYPES16[q.dtype]
+    if offsets is None:
         most = 1
+    elif most is None:
+        most = max(1, T)
     if out is None:
         out = q.new_empty((T, HQ, D)) if stream is None else _new(stream, q, (T, HQ, D), q.dtype)
     elif not (_plain(out, q.get_device(), q.dtype) and out.shape == (T, HQ, D)):
