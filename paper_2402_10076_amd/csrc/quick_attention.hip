@@ -104,7 +104,9 @@ __device__ __forceinline__ void load_values(ValueWords<D>& w, const uint8_t* pag
 // T = min(D, 128) / 16.
 template <int D>
 struct Column {
-    float m, l;
+    Reference ref;
+    bool away;      // whether it is further than this form of the loop goes
+    float l;
     f4_t o[D / 16];
 };
 
@@ -162,7 +164,7 @@ __device__ __forceinline__ void score(const KeyWords<D>& w, const u4_t (&q)[NC][
 }
 
 // The weights of those, as operands p[n][r] of 32 tokens each.
-template <int DT, int D, int NC>
+template <int DT, int D, int NC, bool FAR>
 __device__ __forceinline__ void weigh(f4_t (&s)[NC][4], Column<D> (&col)[NC], const Seen (&seen)[NC], int token0, bool masked,
                                       bool ok, float scale, int lane, u4_t (&p)[NC][2])
 {
@@ -183,23 +185,24 @@ __device__ __forceinline__ void weigh(f4_t (&s)[NC][4], Column<D> (&col)[NC], co
         for (int i = 0; i < 4; i++)
 #pragma unroll
             for (int e = 0; e < 4; e++) top = fmaxf(top, s[n][i][e]);
-        top *= scale;
-        if (__ballot(top > col[n].m + kRoom)) {
+        if (FAR || __ballot(fmaf(top, scale, -col[n].ref.m) > kRoom)) {
             seldom();
             top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
-            const float m = top > col[n].m + kRoom ? top - kLift : col[n].m;
-            const float f = __builtin_amdgcn_exp2f(col[n].m - m);
-            col[n].m = m;
+            const float f = col[n].ref.template raise<FAR>(top, scale, col[n].away);
             col[n].l *= f;
 #pragma unroll
             for (int j = 0; j < D / 16; j++) col[n].o[j] *= f;
+        }
+        if constexpr (FAR) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) s[n][i] -= col[n].ref.base;
         }
 #pragma unroll
         for (int i = 0; i < 4; i++)
 #pragma unroll
             for (int e = 0; e < 4; e += 2) {
-                const float u = __builtin_amdgcn_exp2f(fmaf(s[n][i][e], scale, -col[n].m));
-                const float v = __builtin_amdgcn_exp2f(fmaf(s[n][i][e + 1], scale, -col[n].m));
+                const float u = __builtin_amdgcn_exp2f(fmaf(s[n][i][e], scale, -col[n].ref.m));
+                const float v = __builtin_amdgcn_exp2f(fmaf(s[n][i][e + 1], scale, -col[n].ref.m));
                 col[n].l += u + v;
                 p[n][i / 2][i % 2 * 2 + e / 2] = pair16<DT>(u, v);
             }
@@ -299,8 +302,11 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
 {
     typedef Kv4<D> L;
     constexpr int BC = 16 * NC, KW = D / 32, TILES = (D < 128 ? D : 128) / 16, ROW = D + 4;
+    // where registers are short the last step's addresses are not kept over the loop (64 channels: 67.8 us for 64.8 with
+    // four of them in scratch; with 128, which have registers left, drafts take 26.2 for 25.3 so)
+    constexpr bool LATE = !WHOLE && ((D == 64 && NC == 1) || D > 128);
     __shared__ float sums[WAVES][16][ROW];
-    __shared__ float refs[WAVES][16][2];
+    __shared__ float refs[WAVES][16][3];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int worker = blockIdx.x;
     Walk walk;
@@ -357,10 +363,6 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
             const int pos = t.base + of[n];
             seen[n].hi = a.s.causal ? min(pos + 1, t.length) : t.length;
             seen[n].lo = a.s.window ? max(0, pos + 1 - a.s.window) : 0;
-            col[n].m = kNothing;
-            col[n].l = 0;
-#pragma unroll
-            for (int j = 0; j < D / 16; j++) col[n].o[j] = f4_t{0, 0, 0, 0};
         }
         const uint8_t* head = a.cache + walk.h * L::kBytes;
         const uint32_t stride = a.s.heads * L::kBytes;
@@ -370,49 +372,83 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
             inside = x >= 0 && x < a.pages;
             return head + (int64_t)(inside ? x : 0) * stride;
         };
-        KeyWords<D> keys;
-        ValueWords<D> values;
-        bool ok = false;
-        const uint8_t* page = a.cache;
-        if (count) {
-            page = page_of(0, ok);
-            load_keys<D>(keys, page, lane);
-            load_values<D>(values, page, lane);
-        }
-        if (a.q_sign) {
-            seldom();
+        auto all_pages = [&](auto form) {
+            constexpr bool FAR = decltype(form)::far;
 #pragma unroll
-            for (int n = 0; n < NC; n++)
+            for (int n = 0; n < NC; n++) {
+                col[n].ref = kNoReference;
+                col[n].away = false;
+                col[n].l = 0;
 #pragma unroll
-                for (int j = 0; j < KW; j++) q[n][j] ^= a.q_sign;
-        }
-        for (int n = 0; n < count; n++) {
-            const int token0 = (p0 + wave + WAVES * n) * kPage;
-            const bool masked = token0 + kPage > t.all_hi || token0 < t.all_lo || !ok;
-            f4_t s[NC][4];
-            u4_t p[NC][2];
-            score<DT, D, NC>(keys, q, s);
-            // the next page's keys and values take the place of this one's as those are done with (the last one's again)
-            bool next_ok;
-            const uint8_t* next = page_of(min(n + 1, count - 1), next_ok);
-            load_keys<D>(keys, next, lane);
-            weigh<DT, D, NC>(s, col, seen, token0, masked, ok, a.scale, lane, p);
-            uint32_t mark = 0;
-#pragma unroll
-            for (int h = 0; h < ValueWords<D>::HALVES; h++)
-#pragma unroll
-                for (int i = 0; i < 4; i++) mark |= beyond<DT>(values.s[h][i]);
-            if (__ballot(mark != 0)) {
+                for (int j = 0; j < D / 16; j++) col[n].o[j] = f4_t{0, 0, 0, 0};
+            }
+            KeyWords<D> keys;
+            ValueWords<D> values;
+            bool ok = false;
+            const uint8_t* page = a.cache;
+            if (!FAR && count) {
+                page = page_of(0, ok);
+                load_keys<D>(keys, page, lane);
+                load_values<D>(values, page, lane);
+            }
+            if (!FAR && a.q_sign) {
                 seldom();
 #pragma unroll
-                for (int x = 0; x < NC; x++)
-                    spoil<DT, D>(col[x], page, seen[x].lo - token0, ok ? seen[x].hi - token0 : 0, lane);
-                take_out<DT, D>(values);
+                for (int n = 0; n < NC; n++)
+#pragma unroll
+                    for (int j = 0; j < KW; j++) q[n][j] ^= a.q_sign;
             }
-            add_values<DT, D, NC>(values, p, col);
-            load_values<D>(values, next, lane);
-            page = next;
-            ok = next_ok;
+            for (int n = 0; n < count; n++) {
+                if (FAR) {
+                    page = page_of(n, ok);
+                    load_keys<D>(keys, page, lane);
+                }
+                const int token0 = (p0 + wave + WAVES * n) * kPage;
+                const bool masked = token0 + kPage > t.all_hi || token0 < t.all_lo || !ok;
+                f4_t s[NC][4];
+                u4_t p[NC][2];
+                score<DT, D, NC>(keys, q, s);
+                // the next page's keys and values take the place of this one's as those are done with (the last one's again)
+                bool next_ok = false;
+                const uint8_t* next = page;
+                if (!FAR) {
+                    next = page_of(min(n + 1, count - 1), next_ok);
+                    load_keys<D>(keys, next, lane);
+                }
+                weigh<DT, D, NC, FAR>(s, col, seen, token0, masked, ok, a.scale, lane, p);
+                if (FAR) {
+                    seldom();
+                    load_values<D>(values, page, lane);
+                }
+                uint32_t mark = 0;
+#pragma unroll
+                for (int h = 0; h < ValueWords<D>::HALVES; h++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) mark |= beyond<DT>(values.s[h][i]);
+                if (__ballot(mark != 0)) {
+                    seldom();
+#pragma unroll
+                    for (int x = 0; x < NC; x++)
+                        spoil<DT, D>(col[x], page, seen[x].lo - token0, ok ? seen[x].hi - token0 : 0, lane);
+                    take_out<DT, D>(values);
+                }
+                add_values<DT, D, NC>(values, p, col);
+                if (!FAR) {
+                    load_values<D>(values, next, lane);
+                    page = next;
+                    ok = next_ok;
+                }
+            }
+        };
+        all_pages(Near{});
+        // far scores: this wave's pages again, one after the other
+        bool away = false;
+#pragma unroll
+        for (int n = 0; n < NC; n++) away |= col[n].away;
+        if (__builtin_expect(__ballot(away) != 0, 0)) {
+            seldom();
+            if (!WHOLE) ids = table[min(p0 + wave + WAVES * lane, p1 - 1)];
+            all_pages(Far{});
         }
         const bool whole = walk.at == 0 && take == t.cost;
         const int64_t slot = 2 * worker + (first ? 0 : 1);
@@ -424,8 +460,9 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
             if (n || !first) __syncthreads();
             const float l = over_groups(col[n].l, [](float x, float y) { return x + y; });
             if (g == 0) {
-                refs[wave][c][0] = col[n].m;
-                refs[wave][c][1] = l;
+                refs[wave][c][0] = col[n].ref.m;
+                refs[wave][c][1] = col[n].ref.base;
+                refs[wave][c][2] = l;
             }
 #pragma unroll
             for (int h = 0; h < ValueWords<D>::HALVES; h++)
@@ -439,17 +476,19 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
                 }
             __syncthreads();
             constexpr int PIECES = D / 8;
-            for (int at = threadIdx.x; at < 16 * PIECES; at += 64 * WAVES) {
+            for (int at = LATE ? late(threadIdx.x) : threadIdx.x; at < 16 * PIECES; at += 64 * WAVES) {
                 const int x = at / PIECES, d = at % PIECES * 8, cc = walk.j * BC + n * 16 + x;
                 if (cc >= t.columns) continue;
-                float m = refs[0][x][0];
+                auto of_wave = [&](int w) { return Reference{refs[w][x][0], refs[w][x][1]}; };
+                Reference most = of_wave(0);
 #pragma unroll
-                for (int w = 1; w < WAVES; w++) m = fmaxf(m, refs[w][x][0]);
+                for (int w = 1; w < WAVES; w++)
+                    if (of_wave(w).above(most, a.scale) > 0) most = of_wave(w);
                 float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0;
 #pragma unroll
                 for (int w = 0; w < WAVES; w++) {
-                    const float f = __builtin_amdgcn_exp2f(refs[w][x][0] - m);
-                    sum += refs[w][x][1] * f;
+                    const float f = __builtin_amdgcn_exp2f(of_wave(w).above(most, a.scale));
+                    sum += refs[w][x][2] * f;
 #pragma unroll
                     for (int j = 0; j < 8; j++) v[j] += sums[w][x][d + j] * f;
                 }
@@ -457,15 +496,12 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
                     const int i = cc * a.group_inv >> 16;
                     const int64_t row = (int64_t)(t.first + i) * (a.s.heads * a.s.group) + walk.h * a.s.group + cc - i * a.s.group;
                     *(u4_t*)(a.out + 2 * (row * D + d)) = rounded8<DT>(v, sum == 0 ? 0.0f : 1.0f / sum);
-                    if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
+                    if (a.lse && d == 0) a.lse[row] = most.log_sum(sum, a.scale);
                 } else {
-                    float* to = a.part + ((slot * BC + n * 16 + x) * D + d);
+                    float* to = a.part + (slot * BC + n * 16 + x) * D + d;
                     *(f4_t*)to = f4_t{v[0], v[1], v[2], v[3]};
                     *(f4_t*)(to + 4) = f4_t{v[4], v[5], v[6], v[7]};
-                    if (d == 0) {
-                        a.part_ml[(slot * BC + n * 16 + x) * 2] = m;
-                        a.part_ml[(slot * BC + n * 16 + x) * 2 + 1] = sum;
-                    }
+                    if (d == 0) a.part_ref[slot * BC + n * 16 + x] = f4_t{most.m, most.base, sum, 0};
                 }
             }
         }
@@ -481,10 +517,9 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
 }
 
 // Joins the parts of the item that a worker left unfinished: its own, and the
-// first ones of the workers after it.  A thread has eight channels of a column;
-// the parts' references first, so that the loads of their sums are independent
-// of each other.  A launch and a chain of three loads: 4.6 us (decode), 15 (8192
-// queries of 64 heads, 29 MB).
+// first ones of the workers after it.  A thread has eight channels of a column.
+// A launch and a chain of two loads: 4.4 us (drafts; with the references in a
+// pass of their own 4.8), 13 (8192 queries of 64 heads, 29 MB).
 template <int DT, int D, int BC>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
@@ -496,28 +531,46 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
     const int at = threadIdx.x + 256 * blockIdx.y, x = at / PIECES, d = at % PIECES * 8, cc = col0 + x;
     if (x >= BC || cc >= columns) return;
     auto place = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (worker + i)) * BC + x; };
-    float m = kNothing;
-#pragma unroll 4
-    for (int i = 0; i < parts; i++) m = fmaxf(m, a.part_ml[place(i) * 2]);
+    // some parts at a time, their loads under way together (behind the last one that again, which adds nothing): with few
+    // columns a long sequence has many
+    constexpr int STEP = BC == 16 ? 4 : 2;
+    Reference most = kNoReference;
     float sum = 0, v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-    for (int i = 0; i < parts; i++) {
-        const int64_t p = place(i);
-        const float* ml = a.part_ml + p * 2;
-        const f4_t* from = (const f4_t*)(a.part + p * D + d);
-        const f4_t u = from[0], w = from[1];
-        const float f = __builtin_amdgcn_exp2f(ml[0] - m);
-        sum += ml[1] * f;
+    for (int i = 0; i < parts; i += STEP) {
+        f4_t r[STEP], u[STEP], w[STEP];
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-            v[k] += u[k] * f;
-            v[4 + k] += w[k] * f;
+        for (int j = 0; j < STEP; j++) {
+            const int64_t p = place(min(i + j, parts - 1));
+            const f4_t* from = (const f4_t*)(a.part + p * D + d);
+            r[j] = a.part_ref[p];
+            u[j] = from[0];
+            w[j] = from[1];
+        }
+        const Reference before = most;
+#pragma unroll
+        for (int j = 0; j < STEP; j++) {
+            const Reference x{r[j][0], r[j][1]};
+            if (x.above(most, a.scale) > 0) most = x;
+        }
+        const float g = __builtin_amdgcn_exp2f(before.above(most, a.scale));
+        sum *= g;
+#pragma unroll
+        for (int k = 0; k < 8; k++) v[k] *= g;
+#pragma unroll
+        for (int j = 0; j < STEP; j++) {
+            const float f = i + j < parts ? __builtin_amdgcn_exp2f(Reference{r[j][0], r[j][1]}.above(most, a.scale)) : 0.0f;
+            sum += r[j][2] * f;
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                v[k] += u[j][k] * f;
+                v[4 + k] += w[j][k] * f;
+            }
         }
     }
     const int i = cc / a.s.group;
     const int64_t row = (int64_t)(first + i) * (a.s.heads * a.s.group) + h * a.s.group + cc - i * a.s.group;
     *(u4_t*)(a.out + 2 * (row * D + d)) = rounded8<DT>(v, sum == 0 ? 0.0f : 1.0f / sum);
-    if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
+    if (a.lse && d == 0) a.lse[row] = most.log_sum(sum, a.scale);
 }
 
 // Most columns of a sequence.
@@ -619,7 +672,7 @@ extern "C" size_t quick_kv4_attention_workspace_bytes(const quick_attention_t* p
 {
     if (!p || check_attention(*p) || p->T == 0 || p->seqs == 0 || whole_items(*p)) return 0;
     const size_t w = (size_t)workers_of(*p), c = (size_t)columns_of(*p);
-    return w * 32 + 2 * w * c * ((size_t)p->D + 2) * sizeof(float);
+    return w * 32 + 2 * w * c * ((size_t)p->D + 4) * sizeof(float);
 }
 
 extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, int dtype, const void* cache, const int32_t* table,
@@ -663,7 +716,7 @@ extern "C" int quick_kv4_attention(const quick_attention_t* p, const void* q, in
     if (need) {
         a.joins = (int32_t*)workspace;
         a.part = (float*)((uint8_t*)workspace + (size_t)a.workers * 32);
-        a.part_ml = a.part + 2 * (size_t)a.workers * columns * p->D;
+        a.part_ref = (f4_t*)(a.part + 2 * (size_t)a.workers * columns * p->D);
     }
     a.q_token = p->q_token;
     a.q_head = p->q_head;

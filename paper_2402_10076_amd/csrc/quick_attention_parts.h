@@ -11,13 +11,68 @@ typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 typedef float f16_t __attribute__((ext_vector_type(16)));
 
+// Keeps a seldom taken branch a branch: the compiler would rather work both
+// sides out and select.
+__device__ __forceinline__ void seldom() { asm volatile("" ::); }
+// v, of which the compiler then knows nothing: addresses made of it are worked out
+// where they are used and hold no registers through a loop before that.
+__device__ __forceinline__ int late(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // Softmax weights are 2^(s - m), m within a reference of the scores seen so
 // far: set kLift below their largest, and again only when one passes it by
 // kRoom, so that most pages need no exchange between lanes and no rescaling.
 // Weights are then at most 2^kRoom, which f16 holds, and those down to
 // 2^-(24 + kLift) of the largest still count in it.
 constexpr float kLift = 6.0f, kRoom = 14.0f;
-constexpr float kNothing = -3.0e38f;   // a reference before any score
+constexpr float kNothing = -3.4028234663852886e38f;   // a reference before any score (the least number)
+
+// A column's reference.  A weight's exponent is fma(score, scale, -m), rounded
+// once, so it is the same function of the score for every token, whatever m is,
+// and whether one passes kRoom is asked of that value itself.  But m, a binary32
+// number, comes no nearer to a score than half its last place.  Where one is to
+// pass kFar (whose last place is 2^-3) the pages are gone through again in a form
+// of the loop for far scores: it takes them less `base`, the column's largest when
+// its reference was set, with m = -kLift.  (base is zero otherwise.)  In one form
+// for both a base cost 2 to 5 % of calls of 64 and of 256 channels.
+constexpr float kFar = 1048576.0f;
+struct Reference {
+    float m, base;
+
+    // To the column's largest score, if its weight has passed the room.  Returns what the sums so far are multiplied
+    // by.  Without FAR away is set where that needs a base.
+    template <bool FAR>
+    __device__ __forceinline__ float raise(float top, float scale, bool& away)
+    {
+        const bool up = fmaf(FAR ? top - base : top, scale, -m) > kRoom;
+        const float near = fmaf(top, scale, -kLift);
+        const bool far = fabsf(near) > kFar;
+        Reference to = *this;
+        if (up) to = FAR && far ? Reference{-kLift, top} : Reference{near, 0.0f};
+        const float f = __builtin_amdgcn_exp2f(FAR ? above(to, scale) : m - to.m);
+        *this = to;
+        away |= !FAR && up && far;
+        return f;
+    }
+    // How far this one lies above another.
+    __device__ __forceinline__ float above(const Reference& o, float scale) const { return fmaf(base - o.base, scale, m - o.m); }
+    // Logarithm of a sum of weights.
+    __device__ __forceinline__ float log_sum(float l, float scale) const
+    {
+        return l == 0 ? -INFINITY : (fmaf(base, scale, m) + __log2f(l)) * 0.69314718055994531f;
+    }
+};
+constexpr Reference kNoReference{kNothing, 0.0f};
+// The forms of a loop over pages.
+struct Near {
+    static constexpr bool far = false;
+};
+struct Far {
+    static constexpr bool far = true;
+};
 
 struct AttnArgs {
     AttnShape s;
@@ -27,7 +82,7 @@ struct AttnArgs {
     uint8_t* out;
     float* lse;
     float* part;          // [2 * workers][columns][D] sums of a part of an item's pages
-    float* part_ml;       // [2 * workers][columns][2] their references and sums of weights
+    f4_t* part_ref;       // [2 * workers][columns] their references (m, base) and sums of weights
     int32_t* joins;       // [workers][8] the item that a worker leaves unfinished
     int64_t q_token, q_head;
     int32_t pages, workers;
@@ -71,9 +126,6 @@ __device__ __forceinline__ uint32_t pair16(float a, float b)
     if constexpr (DT == QUICK_F16) return bits_as<uint32_t>(__builtin_convertvector((f2_t{a, b}), h2_t));
     else return bits_as<uint32_t>(__builtin_convertvector((f2_t{a, b}), b2_t));
 }
-// Keeps a seldom taken branch a branch: the compiler would rather work both
-// sides out and select.
-__device__ __forceinline__ void seldom() { asm volatile("" ::); }
 // The scale that byte i of a word of scales stands for, for code_pair: its byte is
 // the exponent.  The conversion reads nothing else of a scale (tried with every
 // code, exponent and 64 patterns of the other bits), so those hold what comes.

@@ -184,11 +184,15 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
 {
     typedef Kv4<D> L;
     constexpr int BC = 32 * NW, KS = D / 16, VT = D / 32, T = (D < 128 ? D : 128) / 16;
+    // the last step's addresses are not kept over the loop, which leaves them no registers (with 64 channels it does, and
+    // a window's many items take 78.5 us for 76.5 so)
+    constexpr bool LATE = D > 64;
     __shared__ Tiles<D> tiles[NB];
+    __shared__ uint32_t aways[2][NW];   // whether a wave of this item (of the next one) has met far scores
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5;
     const int worker = blockIdx.x;
     Walk walk = find_share<BC, true>(a.s, a.workers, worker, kTiledShare);
-    int join[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    int join[8] = {0, 0, 0, 0, 0, 0, 0, 0}, odd = 0;
     for (bool first = true; walk.left > 0 && walk.b < a.s.seqs; first = false) {
         const Tile t = tile_of<BC>(a.s, walk.b, walk.j);
         const int take = (int)min((int64_t)(t.cost - walk.at), walk.left);
@@ -208,12 +212,10 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
 #pragma unroll
             for (int s = 0; s < KS; s++) q[s] = *(const u4_t*)(from + s * 32);
         }
-        float m = kNothing, l = 0;
+        Reference ref;
+        bool away = false;
+        float l;
         f16_t o[VT];
-#pragma unroll
-        for (int j = 0; j < VT; j++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) o[j][r] = 0;
         const int32_t* table = a.table + (int64_t)walk.b * a.s.width;
         const uint8_t* head_of_cache = a.cache + walk.h * L::kBytes;
         const uint32_t stride = a.s.heads * L::kBytes;
@@ -238,7 +240,8 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             for (int k = 0; k < KS; k++) s = mfma32<DT>(w.k[x][k][lane], q[k], s);
         };
         // hides what a column does not see of those, and sets its reference
-        auto refer = [&](f16_t& s, int token0, bool ok) {
+        auto refer = [&](auto form, f16_t& s, int token0, bool ok) {
+            constexpr bool FAR = decltype(form)::far;
             if (token0 + 32 > t.all_hi || token0 < t.all_lo || !ok) {
                 seldom();
                 const int from = token0 + 4 * half;
@@ -249,18 +252,18 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             float top = s[0];
 #pragma unroll
             for (int r = 0; r < 16; r++) top = fmaxf(top, s[r]);
-            top *= a.scale;
-            if (__ballot(top > m + kRoom)) {
+            if (FAR || __ballot(fmaf(top, a.scale, -ref.m) > kRoom)) {
                 seldom();
-                top = fmaxf(top, swapped_halves(top, lane));
-                const float to = top > m + kRoom ? top - kLift : m;
-                const float f = __builtin_amdgcn_exp2f(m - to);
-                m = to;
+                const float f = ref.raise<FAR>(fmaxf(top, swapped_halves(top, lane)), a.scale, away);
                 l *= f;
 #pragma unroll
                 for (int j = 0; j < VT; j++)
 #pragma unroll
                     for (int r = 0; r < 16; r++) o[j][r] *= f;
+            }
+            if constexpr (FAR) {
+#pragma unroll
+                for (int r = 0; r < 16; r++) s[r] -= ref.base;
             }
         };
         // Half x of page w: s's weights and the values they weigh; beside them the scores s1 of half x1 of page w1.
@@ -285,8 +288,8 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
                 else f[k % AHEAD] = w.v[2 * x + (k + AHEAD - KS) / VT][(k + AHEAD - KS) % VT][lane];
 #pragma unroll
                 for (int r = 16 * k / KS / 2 * 2; r < 16 * (k + 1) / KS / 2 * 2; r += 2) {
-                    const float u = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -m));
-                    const float v = __builtin_amdgcn_exp2f(fmaf(s[r + 1], a.scale, -m));
+                    const float u = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -ref.m));
+                    const float v = __builtin_amdgcn_exp2f(fmaf(s[r + 1], a.scale, -ref.m));
                     l += u + v;
                     p[r / 8][r % 8 / 2] = pair16<DT>(u, v);
                 }
@@ -301,6 +304,20 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
+        auto begin = [&] {
+            ref = kNoReference;
+            l = 0;
+#pragma unroll
+            for (int j = 0; j < VT; j++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) o[j][r] = 0;
+        };
+        // blocks of a page that the type cannot hold
+        auto see_bad = [&](const Tiles<D>& w, const uint8_t* page, int token0, bool ok) {
+            const u4_t bad = *(const u4_t*)w.bad;
+            if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) spoil<DT, D>(o, page, lo - token0, (ok ? hi : 0) - token0, lane);
+        };
+        begin();
         const uint8_t *page = a.cache, *page1 = a.cache;
         bool ok = false;
         f16_t s;
@@ -351,7 +368,7 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             };
             if (work) {
                 first_operands(w, 1);
-                refer(s, token0, ok);
+                refer(Near{}, s, token0, ok);
                 if constexpr (NB > 2) half_page(w, 0, s, w, 1, s1, on);
                 else half_page(w, 0, s, w, 1, s1, [](int) {});
             } else if (NB > 2) all_on();
@@ -363,23 +380,59 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             __syncthreads();
             if (work) {
                 first_operands(tiles[to], 0);
-                refer(s1, token0 + 32, ok);
+                refer(Near{}, s1, token0 + 32, ok);
                 half_page(w, 1, s1, tiles[to], 0, s, [](int) {});
-                const u4_t bad = *(const u4_t*)w.bad;
-                if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) spoil<DT, D>(o, page, lo - token0, (ok ? hi : 0) - token0, lane);
+                see_bad(w, page, token0, ok);
             }
             ok = ok1;
             page = page1;
             at = to;
         }
         // the next item's first page goes where the last one's lies
+        const uint32_t gone = __ballot(away) != 0;
+        aways[odd][wave] = gone;     // (every lane the same)
         __syncthreads();
+        uint32_t any = 0;
+#pragma unroll
+        for (int w = 0; w < NW; w++) any |= aways[odd][w];
+        odd ^= 1;
+        if (__builtin_expect(uniform(any) != 0, 0)) {
+            // far scores: the pages again, one after the other
+            seldom();
+            begin();
+            for (int n = 0; n < count; n++) {
+                const Tiles<D>& w = tiles[0];
+                const int token0 = (p0 + n) * kPage;
+                id = table[p0 + n];
+                fetch(n);
+                Unstage<DT, D, NW> un;
+                un.template step<0>(next, tiles[0], wave, lane);
+                un.template step<1>(next, tiles[0], wave, lane);
+                un.template step<2>(next, tiles[0], wave, lane);
+                un.template step<3>(next, tiles[0], wave, lane);
+                __syncthreads();
+                if (work) {
+#pragma unroll 1
+                    for (int x = 0; x < 2; x++) {
+                        // (the scores beside the weights are these again)
+                        scores(w, x, s);
+                        first_operands(w, x);
+                        refer(Far{}, s, token0 + 32 * x, next_ok);
+                        f16_t again;
+                        half_page(w, x, s, w, x, again, [](int) {});
+                    }
+                    see_bad(w, next_page, token0, next_ok);
+                }
+                __syncthreads();
+            }
+        }
         const bool whole = walk.at == 0 && take == t.cost;
         const int64_t slot = 2 * worker + (first ? 0 : 1);
         if (walk.at == 0 && !whole) {
             set_join(join, walk, t, BC, take, (int)slot);
         }
         if (live) {
+            const int lane = LATE ? late(threadIdx.x & 63) : threadIdx.x & 63, half = lane >> 5;
             l += swapped_halves(l, lane);
             const int64_t row = (int64_t)(t.first + i) * (a.s.heads * a.s.group) + head;
             const float f = !whole ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
@@ -404,10 +457,8 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
                         }
                     }
             if (half == 0) {
-                if (!whole) {
-                    a.part_ml[(slot * BC + wave * 32 + lane) * 2] = m;
-                    a.part_ml[(slot * BC + wave * 32 + lane) * 2 + 1] = l;
-                } else if (a.lse) a.lse[row] = l == 0 ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+                if (!whole) a.part_ref[slot * BC + wave * 32 + lane] = f4_t{ref.m, ref.base, l, 0};
+                else if (a.lse) a.lse[row] = ref.log_sum(l, a.scale);
             }
         }
         advance<BC, true>(a.s, walk, t, take);

@@ -1,0 +1,106 @@
+"""Attention over the paged 4-bit cache at the ends of its numbers: scores far
+from zero, against the binary64 form.  Every score is exact in binary32 (one
+channel of q and k is not zero), so a row's weights are as exact as the scores'
+differences are, however far the scores lie."""
+import math
+
+import pytest
+import torch
+
+import attn_util as A
+import paper_2402_10076_amd as Q
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+# (D, heads, group, lengths, new, width): by a wave's pages, 16 columns and 32, whole and shared out; through LDS, 128
+# columns and 256; the last ones over many workgroups
+FORMS = [(64, 2, 4, [300, 70], [1, 1], None), (128, 2, 8, [300, 1, 64], [1, 1, 1], None), (256, 1, 4, [300, 9], [4, 2], None),
+         (128, 1, 8, [300, 200], [4, 3], None), (64, 1, 4, [300, 200], [8, 3], 70), (128, 2, 4, [4400, 200], [2, 1], 70),
+         (128, 1, 16, [2400, 200], [8, 3], 70), (256, 1, 16, [1400, 200], [2, 3], 70), (64, 1, 8, [300, 70], [100, 20], None),
+         (128, 2, 8, [900, 70], [40, 20], None), (256, 1, 8, [300, 170], [40, 20], None), (64, 1, 8, [400, 70], [300, 20], None),
+         (128, 1, 8, [900, 70], [300, 20], None)]
+
+
+class Exact:
+    """Keys of one channel that are a power of two or one and a half times it, queries of that channel that differ from
+    head to head, normal values."""
+
+    def __init__(self, D, heads, group, lengths, new, width, dtype, q_values, order, top):
+        g = A.gen(51, D, heads, group, sum(lengths))
+        self.dtype, self.group, self.lengths = A.TYPES[dtype], group, lengths
+        need = [-(-n // 64) for n in lengths]
+        ids = torch.randperm(sum(need) + 1, generator=g)
+        self.table = torch.zeros((len(lengths), width or max(need)), dtype=torch.int32)
+        self.cache = Q.kv4_cache(sum(need) + 1, heads, D)
+        self.k, self.v = [], []
+        at = 0
+        for b, n in enumerate(lengths):
+            self.table[b, :need[b]] = ids[at:at + need[b]]
+            at += need[b]
+            # sizes from 2^-6 to 2^top over the sequence, in runs of equal ones
+            size = (torch.arange(n) * (2 * (top + 6) + 1) // max(n, 1)) - 12
+            if order == "falling":
+                size = size.flip(0)
+            elif order == "mixed":
+                size = size[torch.randperm(n, generator=g)]
+            value = torch.where(size % 2 == 0, 1.0, 1.5) * 2.0 ** torch.div(size, 2, rounding_mode="floor")
+            k = torch.zeros(n, heads, D)
+            k[:, :, D - 3] = value.view(-1, 1)
+            k, v = k.to(self.dtype), A.normal(g, n, heads, D, dtype=self.dtype)
+            t = torch.arange(n)
+            slots = (self.table[b, t // 64].long() * 64 + t % 64).to(torch.int32)
+            Q.kv4_write(self.cache, k.cuda(), v.cuda(), slots.cuda())
+            self.k.append(A.rounded(k))
+            assert torch.equal(self.k[b], k.double())
+            self.v.append(A.rounded(v))
+        self.offsets = [0]
+        for n in new:
+            self.offsets.append(self.offsets[-1] + n)
+        self.q = torch.zeros(self.offsets[-1], heads * group, D, dtype=self.dtype)
+        pick = torch.tensor(q_values)[torch.arange(heads * group) * 7 % len(q_values)]
+        self.q[:, :, D - 3] = pick.to(self.dtype)
+        self.most = max(new)
+
+    def check(self, scale, window=0):
+        off = torch.tensor(self.offsets, dtype=torch.int32).cuda()
+        lse = torch.zeros(self.q.shape[:2], device="cuda")
+        out = Q.kv4_attention(self.q.cuda(), self.cache, self.table.cuda(), torch.tensor(self.lengths, dtype=torch.int32).cuda(),
+                              offsets=off, most=self.most, scale=scale, window=window, lse=lse).cpu().double()
+        args = self.lengths, self.offsets, self.group, self.dtype, scale, window
+        want, want_lse, _ = A.attention(self.q.double(), self.k, self.v, *args)
+        size, _, _ = A.attention(self.q.double(), self.k, [v.abs() for v in self.v], *args)
+        assert out.isfinite().all(), "%d of %d rows" % ((~out.isfinite()).any(2).sum(), out.shape[0] * out.shape[1])
+        # A weight's exponent, of 64 at most where it counts, is rounded once (2^-19) and its reference's changes once a
+        # page; the scale's rounding counts for the score's distance from the largest (64 * 2^-23); weights and sums as
+        # elsewhere (half a step of the type; 2^-23 a token), f16's below its normal range too.
+        step, n = A.STEP[self.dtype], max(self.lengths)
+        far = (2.0 ** -19 * (n // 64 + 8) + 2.0 ** -17) * math.log(2)
+        tol = size * (step + 2 * far + n * 2.0 ** -23) + n * 2.0 ** -31 * 6 + want.abs() * step + 2.0 ** -25
+        err = (out - want).abs()
+        assert bool((err <= tol).all()), "err %.3g, of the bound %.3g" % (float(err.max()), float((err / tol).max()))
+        err = (lse.cpu().double() - want_lse).abs()
+        assert bool((err <= want_lse.abs() * 2.0 ** -21 + 2.0 ** -12).all()), float(err.max())
+
+
+@pytest.mark.parametrize("order", ["rising", "falling", "mixed"])
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(map(str, f[:3])) + "-%d-%d" % (f[3][0], f[4][0]))
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_scores_far_from_zero(dtype, form, order):
+    """Up to 2^30 (bfloat16: 2^72) of either sign, beside heads of ordinary ones, whose references move meanwhile."""
+    say("far scores", dtype, form, order)
+    q = [2.0 ** 14, 1.0, -(2.0 ** 13), 2.0 ** -3, 2.0 ** 10, -0.25, 0.0] if dtype == "f16" else \
+        [2.0 ** 58, 1.0, -(2.0 ** 13), 2.0 ** -3, 2.0 ** 10, -(2.0 ** 57), 0.0]
+    b = Exact(*form, dtype, q, order, 14)
+    b.check(1.5)
+    b.check(-1.0, window=150)
+
+
+@pytest.mark.parametrize("form", FORMS[:2] + FORMS[7:10] + FORMS[-1:], ids=lambda f: "-".join(map(str, f[:3])))
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_equal_scores_far_from_zero(dtype, form):
+    """Every token's weight is the same, whatever the score: its product with the scale is not a binary32 number."""
+    say("equal scores", dtype, form)
+    b = Exact(*form, dtype, [1.5 * 2.0 ** e for e in range(-2, 14, 2)], "mixed", -6)
+    for scale in (0.3, 1e3, -7e5, 3e8, 1e20):
+        b.check(scale)
