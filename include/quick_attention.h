@@ -128,8 +128,9 @@ typedef struct quick_attention {
  *   lse      f32 [T][q_heads], log of the sum of exp(scaled scores); NULL = none
  * Products are those of q and of the cached values as `dtype` holds them (a
  * block whose scale it cannot hold, above 2^13 with f16, counts as NaN);
- * scores, softmax and sums are binary32, the weights of the values are rounded
- * to `dtype`, the result once more.  Deterministic.
+ * scores, softmax and sums are binary32 (a sum of values whose magnitudes add up
+ * to 2^128 or more may be infinite), the weights of the values are rounded to
+ * `dtype`, the result once more.  Deterministic.
  * workspace: 16-byte aligned, of quick_kv4_attention_workspace_bytes() (0: may
  * be NULL); calls that share one must be ordered.
  * T < 2^24, q_heads / heads <= 64, seqs <= QUICK_KV4_MAX_SEQS, table_width <

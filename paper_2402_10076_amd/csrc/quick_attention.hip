@@ -185,10 +185,10 @@ __device__ __forceinline__ void weigh(f4_t (&s)[NC][4], Column<D> (&col)[NC], co
         for (int i = 0; i < 4; i++)
 #pragma unroll
             for (int e = 0; e < 4; e++) top = fmaxf(top, s[n][i][e]);
-        if (FAR || __ballot(fmaf(top, scale, -col[n].ref.m) > kRoom)) {
+        if (FAR || __ballot(fmaf(top, scale, -col[n].ref.m) > kRoom<DT>)) {
             seldom();
             top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
-            const float f = col[n].ref.template raise<FAR>(top, scale, col[n].away);
+            const float f = col[n].ref.template raise<DT, FAR>(top, scale, col[n].away);
             col[n].l *= f;
 #pragma unroll
             for (int j = 0; j < D / 16; j++) col[n].o[j] *= f;

@@ -25,9 +25,14 @@ __device__ __forceinline__ int late(int v)
 // Softmax weights are 2^(s - m), m within a reference of the scores seen so
 // far: set kLift below their largest, and again only when one passes it by
 // kRoom, so that most pages need no exchange between lanes and no rescaling.
-// Weights are then at most 2^kRoom, which f16 holds, and those down to
-// 2^-(24 + kLift) of the largest still count in it.
-constexpr float kLift = 6.0f, kRoom = 14.0f;
+// Of f16 weights are then at most 2^14, which it holds, and those down to 2^-30
+// of the largest still count in it.  Bf16 holds far smaller ones, and values near
+// binary32's end, whose products with weights above 1 it could not: there they
+// are at most 1, the first largest 2^-8.
+template <int DT>
+constexpr float kRoom = DT == QUICK_F16 ? 14.0f : 0.0f;
+template <int DT>
+constexpr float kLift = kRoom<DT> - 8.0f;
 constexpr float kNothing = -3.4028234663852886e38f;   // a reference before any score (the least number)
 
 // A column's reference.  A weight's exponent is fma(score, scale, -m), rounded
@@ -44,14 +49,14 @@ struct Reference {
 
     // To the column's largest score, if its weight has passed the room.  Returns what the sums so far are multiplied
     // by.  Without FAR away is set where that needs a base.
-    template <bool FAR>
+    template <int DT, bool FAR>
     __device__ __forceinline__ float raise(float top, float scale, bool& away)
     {
-        const bool up = fmaf(FAR ? top - base : top, scale, -m) > kRoom;
-        const float near = fmaf(top, scale, -kLift);
+        const bool up = fmaf(FAR ? top - base : top, scale, -m) > kRoom<DT>;
+        const float near = fmaf(top, scale, -kLift<DT>);
         const bool far = fabsf(near) > kFar;
         Reference to = *this;
-        if (up) to = FAR && far ? Reference{-kLift, top} : Reference{near, 0.0f};
+        if (up) to = FAR && far ? Reference{-kLift<DT>, top} : Reference{near, 0.0f};
         const float f = __builtin_amdgcn_exp2f(FAR ? above(to, scale) : m - to.m);
         *this = to;
         away |= !FAR && up && far;

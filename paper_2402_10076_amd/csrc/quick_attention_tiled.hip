@@ -252,9 +252,9 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
             float top = s[0];
 #pragma unroll
             for (int r = 0; r < 16; r++) top = fmaxf(top, s[r]);
-            if (FAR || __ballot(fmaf(top, a.scale, -ref.m) > kRoom)) {
+            if (FAR || __ballot(fmaf(top, a.scale, -ref.m) > kRoom<DT>)) {
                 seldom();
-                const float f = ref.raise<FAR>(fmaxf(top, swapped_halves(top, lane)), a.scale, away);
+                const float f = ref.raise<DT, FAR>(fmaxf(top, swapped_halves(top, lane)), a.scale, away);
                 l *= f;
 #pragma unroll
                 for (int j = 0; j < VT; j++)

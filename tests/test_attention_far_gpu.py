@@ -104,3 +104,29 @@ def test_equal_scores_far_from_zero(dtype, form):
     b = Exact(*form, dtype, [1.5 * 2.0 ** e for e in range(-2, 14, 2)], "mixed", -6)
     for scale in (0.3, 1e3, -7e5, 3e8, 1e20):
         b.check(scale)
+
+
+@pytest.mark.parametrize("exponent", [-90, 120])
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(map(str, f[:3])) + "-%d-%d" % (f[3][0], f[4][0]))
+def test_values_far_from_one(form, exponent):
+    """bfloat16 values near the ends of binary32: a row is a mean of them, and so are the sums of it that are held."""
+    D, heads, group, lengths, new, width = form
+    say("far values", form, exponent)
+    g = A.gen(52, D, heads, sum(lengths))
+    dtype, need = torch.bfloat16, [-(-n // 64) for n in lengths]
+    table = torch.zeros((len(lengths), width or max(need)), dtype=torch.int32)
+    cache, at, ks, vs, offsets = Q.kv4_cache(sum(need), heads, D), 0, [], [], [0]
+    for b, n in enumerate(lengths):
+        table[b, :need[b]] = torch.arange(at, at + need[b])
+        k, v = A.normal(g, n, heads, D, dtype=dtype), (torch.randn(n, heads, D, generator=g) * 2.0 ** exponent).to(dtype)
+        Q.kv4_write(cache, k.cuda(), v.cuda(), torch.arange(at * 64, at * 64 + n, dtype=torch.int32).cuda())
+        at += need[b]
+        ks.append(A.rounded(k))
+        vs.append(A.rounded(v))
+        offsets.append(offsets[-1] + new[b])
+    q = A.normal(g, offsets[-1], heads * group, D, scale=1.5, dtype=dtype)
+    out = Q.kv4_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(),
+                          offsets=torch.tensor(offsets, dtype=torch.int32).cuda(), most=max(new)).cpu().double()
+    want, _, tol = A.attention(q.double(), ks, vs, lengths, offsets, group, dtype)
+    err = (out - want).abs()
+    assert bool((err <= tol).all()), "err %.3g, of the bound %.3g" % (float(err.max()), float((err / tol).max()))
