@@ -126,8 +126,9 @@ typedef struct quick_attention {
  *   out      [T][q_heads][D] of `dtype`, 16-byte aligned, contiguous, must not
  *            overlap q; rows that belong to no sequence keep their values
  *   lse      f32 [T][q_heads], log of the sum of exp(scaled scores); NULL = none
- * Products are those of q and of the cached values as `dtype` holds them (a
- * block whose scale it cannot hold, above 2^13 with f16, counts as NaN);
+ * Products are those of q and of the cached keys and values as `dtype` holds
+ * them (a block whose scale it cannot hold, above 2^13 with f16 and 2^125 with
+ * bf16, counts as NaN);
  * scores, softmax and sums are binary32 (a sum of values whose magnitudes add up
  * to 2^128 or more may be infinite), the weights of the values are rounded to
  * `dtype`, the result once more.  Deterministic.

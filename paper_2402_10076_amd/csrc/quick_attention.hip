@@ -117,14 +117,15 @@ struct Seen {
 
 // The blocks of values that are beyond the type make NaN of the columns that
 // see them, and nothing of the others: they are taken out of the product (their
-// scales become 2^-127) and the sums of those columns set.  Seldom run.
+// scales become 2^-127) and the sums of those columns set.  Seldom run.  (Blocks of
+// keys are NaN by themselves, and what does not see them hides their scores.)
 template <int DT, int D>
 __device__ __forceinline__ void take_out(ValueWords<D>& w)
 {
 #pragma unroll
     for (int h = 0; h < ValueWords<D>::HALVES; h++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) w.s[h][i] &= ~((beyond<DT>(w.s[h][i]) >> 7) * 0xFFu);
+        for (int i = 0; i < 4; i++) w.s[h][i] &= ~whole_bytes(beyond<DT>(w.s[h][i]));
 }
 template <int DT, int D>
 __device__ __forceinline__ void spoil(Column<D>& col, const uint8_t* page, int lo, int hi, int lane)
@@ -150,13 +151,17 @@ __device__ __forceinline__ void spoil(Column<D>& col, const uint8_t* page, int l
 template <int DT, int D, int NC>
 __device__ __forceinline__ void score(const KeyWords<D>& w, const u4_t (&q)[NC][D / 32], f4_t (&s)[NC][4])
 {
+    // (blocks beyond the type get the scale of NaN)
+    uint32_t scales[KeyWords<D>::HALVES];
+#pragma unroll
+    for (int h = 0; h < KeyWords<D>::HALVES; h++) scales[h] = w.s[h] | whole_bytes(beyond<DT>(w.s[h]));
 #pragma unroll
     for (int i = 0; i < 4; i++) {
 #pragma unroll
         for (int n = 0; n < NC; n++) s[n][i] = f4_t{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < D / 32; j++) {
-            const u4_t k = code_words<DT>(w.k[i][j], scale_of(w.s[j / 4], i));
+            const u4_t k = code_words<DT>(w.k[i][j], scale_of(scales[j / 4], i));
 #pragma unroll
             for (int n = 0; n < NC; n++) s[n][i] = mfma16<DT>(k, q[n][j], s[n][i]);
         }

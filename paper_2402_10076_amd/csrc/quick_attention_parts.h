@@ -160,6 +160,8 @@ __device__ __forceinline__ uint32_t beyond(uint32_t w)
 {
     return ((w & 0x7F7F7F7Fu) + (DT == QUICK_F16 ? 0x73737373u : 0x03030303u)) & w & 0x80808080u;
 }
+// 255 where a byte has its bit 7 of those.
+__device__ __forceinline__ uint32_t whole_bytes(uint32_t bits) { return (bits << 1) - (bits >> 7); }
 
 // Eight sums of a column to its row of out.
 template <int DT>

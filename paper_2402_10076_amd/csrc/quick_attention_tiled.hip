@@ -90,7 +90,26 @@ struct Unstage {
     __device__ __forceinline__ void step(Staged<D, NW>& s, Tiles<D>& to, int wave, int lane)
     {
         const int c = lane & 15, g = lane >> 4, x = g & 1, y = g >> 1, w = wave / S::SHARE, part = wave % S::SHARE;
-        if constexpr (STEP == 0) mark = 0;
+        if constexpr (STEP == 0) {
+            // blocks beyond the type: of keys they get the scale of NaN, of values they leave the product
+            mark = 0;
+            uint32_t any = 0;
+#pragma unroll
+            for (int h = 0; h < S::HALVES; h++) any |= beyond<DT>(s.ks[h]) | beyond<DT>(s.vs[h][0]) | beyond<DT>(s.vs[h][1]);
+            if (__ballot(any != 0)) {
+                seldom();
+#pragma unroll
+                for (int h = 0; h < S::HALVES; h++) {
+                    s.ks[h] |= whole_bytes(beyond<DT>(s.ks[h]));
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const uint32_t bits = beyond<DT>(s.vs[h][i]);
+                        mark |= bits;
+                        s.vs[h][i] &= ~whole_bytes(bits);
+                    }
+                }
+            }
+        }
         if constexpr (STEP == 3) {
             const uint64_t any = __ballot(mark != 0);
             to.bad[w] = any != 0;     // (every lane the same)
@@ -107,15 +126,6 @@ struct Unstage {
                 }
             }
             if constexpr (STEP == 1) {
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    mark |= beyond<DT>(s.vs[h][i]);
-                }
-                if (__ballot(mark != 0)) {
-                    seldom();
-#pragma unroll
-                    for (int i = 0; i < 2; i++) s.vs[h][i] &= ~((beyond<DT>(s.vs[h][i]) >> 7) * 0xFFu);
-                }
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     sa[h][e] = scale_of(s.vs[h][0], e);

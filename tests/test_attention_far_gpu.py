@@ -130,3 +130,58 @@ def test_values_far_from_one(form, exponent):
     want, _, tol = A.attention(q.double(), ks, vs, lengths, offsets, group, dtype)
     err = (out - want).abs()
     assert bool((err <= tol).all()), "err %.3g, of the bound %.3g" % (float(err.max()), float((err / tol).max()))
+
+
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(map(str, f[:3])) + "-%d-%d" % (f[3][0], f[4][0]))
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_blocks_beyond_the_type(dtype, form):
+    """A key or value block whose scale q's type cannot hold (of a cache that bfloat16 wrote, or of no writer) is NaN
+    for the rows that see it, in its channels or in all where it is a key's, and nothing for the others."""
+    D, heads, group, lengths, new, width = form
+    say("beyond the type", dtype, form)
+    g = A.gen(53, D, heads, sum(lengths))
+    need = [-(-n // 64) for n in lengths]
+    table = torch.zeros((len(lengths), width or max(need)), dtype=torch.int32)
+    cache, at, offsets = Q.kv4_cache(sum(need), heads, D), 0, [0]
+    for b, n in enumerate(lengths):
+        table[b, :need[b]] = torch.arange(at, at + need[b])
+        Q.kv4_write(cache, *(A.normal(g, n, heads, D, dtype=torch.bfloat16).cuda() for _ in "kv"),
+                    torch.arange(at * 64, at * 64 + n, dtype=torch.int32).cuda())
+        at += need[b]
+        offsets.append(offsets[-1] + new[b])
+    q = A.normal(g, offsets[-1], heads * group, D, scale=1.5, dtype=A.TYPES[dtype])
+    args = q.cuda(), table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda()
+
+    def run(c, **kw):
+        return Q.kv4_attention(args[0], c, *args[1:], offsets=torch.tensor(offsets, dtype=torch.int32).cuda(), most=max(new),
+                               **kw).cpu()
+
+    least, most = (141, 254) if dtype == "f16" else (253, 254)
+    token, block = lengths[0] - 1 - new[0] // 2, D // 32 - 1       # seen by some of the first sequence's rows
+    t = token % 64
+    key = 32 * D + 64 * block + 4 * (t % 16) + t // 16
+    value = 66 * D + 64 * block + 16 * (t % 16 // 4) + 4 * (t // 16) + t % 4
+    for window in (0, 5):
+        ref = run(cache, window=window)
+        assert ref.isfinite().all()
+        for where, scales in ((key, (least, most)), (value, (least, most))):
+            for scale in scales:
+                for h in (0, heads - 1):
+                    bad = cache.clone()
+                    bad[token // 64, h, where] = scale
+                    out = run(bad, window=window)
+                    for row in range(offsets[-1]):
+                        pos = lengths[0] - new[0] + row
+                        sees = row < new[0] and pos >= token and (not window or token > pos - window)
+                        nan = torch.zeros_like(out[row], dtype=torch.bool)
+                        if sees:
+                            nan[h * group:(h + 1) * group, 0 if where == key else 32 * block:] = True
+                        assert torch.equal(out[row].isnan(), nan), (where == key, scale, h, row, window)
+                        same = torch.ones_like(nan[:, 0])
+                        if sees:
+                            same[h * group:(h + 1) * group] = False
+                        assert torch.equal(out[row][same], ref[row][same]), (where == key, scale, h, row, window)
+    # the largest scale that the type holds is one
+    held = cache.clone()
+    held[token // 64, 0, value] = least - 1
+    assert run(held).isfinite().all()
