@@ -523,8 +523,9 @@ __global__ __launch_bounds__(64 * WAVES, stream_resident(D, NC)) void attn_strea
 
 // Joins the parts of the item that a worker left unfinished: its own, and the
 // first ones of the workers after it.  A thread has eight channels of a column.
-// A launch and a chain of two loads: 4.4 us (drafts; with the references in a
-// pass of their own 4.8), 13 (8192 queries of 64 heads, 29 MB).
+// A launch and a chain of two loads, further parts coming while these are added:
+// 4.3 us (drafts), 13 (8192 queries of 64 heads, 29 MB), 11 (64 parts of 200000
+// tokens; 15 with each step's loads when it begins).
 template <int DT, int D, int BC>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
@@ -536,21 +537,31 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
     const int at = threadIdx.x + 256 * blockIdx.y, x = at / PIECES, d = at % PIECES * 8, cc = col0 + x;
     if (x >= BC || cc >= columns) return;
     auto place = [&](int i) { return (int64_t)(i == 0 ? slot0 : 2 * (worker + i)) * BC + x; };
-    // some parts at a time, their loads under way together (behind the last one that again, which adds nothing): with few
-    // columns a long sequence has many
+    // some parts at a time (behind the last one that again, which adds nothing): with few columns a long sequence has many
     constexpr int STEP = BC == 16 ? 4 : 2;
     Reference most = kNoReference;
     float sum = 0, v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int i = 0; i < parts; i += STEP) {
-        f4_t r[STEP], u[STEP], w[STEP];
+    f4_t next[STEP][3];
+    auto load = [&](int i) {
 #pragma unroll
         for (int j = 0; j < STEP; j++) {
             const int64_t p = place(min(i + j, parts - 1));
             const f4_t* from = (const f4_t*)(a.part + p * D + d);
-            r[j] = a.part_ref[p];
-            u[j] = from[0];
-            w[j] = from[1];
+            next[j][0] = a.part_ref[p];
+            next[j][1] = from[0];
+            next[j][2] = from[1];
         }
+    };
+    load(0);
+    for (int i = 0; i < parts; i += STEP) {
+        f4_t r[STEP], u[STEP], w[STEP];
+#pragma unroll
+        for (int j = 0; j < STEP; j++) {
+            r[j] = next[j][0];
+            u[j] = next[j][1];
+            w[j] = next[j][2];
+        }
+        if (i + STEP < parts) load(i + STEP);
         const Reference before = most;
 #pragma unroll
         for (int j = 0; j < STEP; j++) {
