@@ -95,7 +95,8 @@ def lora_add(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
     the tokens of each adapter e, y for those without one; f16 or bf16, a
     [E][rank][K], b [E][N][rank], scales f32 [E] (None: 1), offsets and rows of
     lora_group.  Rows of x, y and out may be apart by any multiple of 8.  out: y
-    itself or another tensor of its shape; a new one if none is given."""
+    itself or another tensor of its shape, whose rows keep their values where
+    ``rows`` does not list them; a new one if none is given, with y's there."""
     what = "lora_add"
     _gpu(what, "x", x)
     code = _type(what, "x", x.dtype, _TYPES16)
@@ -120,7 +121,11 @@ def lora_add(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
         R = rows.shape[0]
         _int32(what, "rows", rows, x, (R,))
     if out is None:
-        out = x.new_empty((T, N)) if stream is None else _new(stream, x, (T, N), x.dtype)
+        if R < T:
+            # the rows that are not listed
+            out = _q._taken(stream, x, lambda: (y.clone(memory_format=torch.contiguous_format),))[0]
+        else:
+            out = x.new_empty((T, N)) if stream is None else _new(stream, x, (T, N), x.dtype)
         ldo = N
     else:
         ldo = _rows(what, "out", out, x, T, N)

@@ -145,3 +145,27 @@ def test_many_slices(T, K, N, E, r):
     say("slices", T, K, N, E, r)
     out = Q.lora_add(y.cuda(), x.cuda(), a.cuda(), b.cuda(), *Q.lora_group(ids.cuda(), E), scales=scales.cuda())
     _check(out, x, y, a, b, ids, scales)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("few", [0, 1, 25])
+@pytest.mark.parametrize("given", [False, True], ids=["current stream", "given stream"])
+def test_rows_that_a_new_result_has_and_the_call_does_not_list(given, few, dtype):
+    """They are y's, whatever the new tensor's memory held."""
+    T, E, N = 40, 3, 64
+    x, y, a, b, ids, _ = _case(10, T, 128, N, E, 8, dtype, bare=False)
+    offsets, rows = Q.lora_group(ids.cuda(), E)
+    dev = [t.cuda() for t in (x, a, b)]
+    wide = torch.zeros((T, N + 8), dtype=x.dtype, device="cuda")
+    wide[:, 8:] = y.cuda()
+    stream = torch.cuda.Stream() if given else torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        left = torch.full((T, N), float("nan"), dtype=x.dtype, device="cuda")     # what the next block of this size holds
+        del left
+    torch.cuda.synchronize()
+    out = Q.lora_add(wide[:, 8:], *dev, offsets.clamp(max=few), rows[:few].contiguous(), stream=stream if given else None)
+    torch.cuda.synchronize()
+    listed = torch.zeros(T, dtype=torch.bool)
+    listed[rows[:few].cpu().long()] = True
+    assert torch.equal(out.cpu()[~listed], y[~listed])
+    _check(out, x, y, a, b, torch.where(listed, ids, -1), None)
