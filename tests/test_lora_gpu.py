@@ -169,3 +169,47 @@ def test_rows_that_a_new_result_has_and_the_call_does_not_list(given, few, dtype
     listed[rows[:few].cpu().long()] = True
     assert torch.equal(out.cpu()[~listed], y[~listed])
     _check(out, x, y, a, b, torch.where(listed, ids, -1), None)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,K,N,E,r", [(27, 512, 1000, 8, 64), (27, 520, 328, 8, 128), (20, 1032, 136, 3, 40), (30, 264, 72, 4, 104),
+                                       (20, 128, 264, 2, 72), (300, 384, 328, 3, 32), (200, 520, 136, 2, 24), (500, 264, 72, 4, 48),
+                                       (160, 256, 136, 2, 96), (1, 4096, 264, 16, 56), (16, 72, 4096, 1, 120)])
+def test_every_rank_with_low_and_high_tiles(T, K, N, E, r, dtype):
+    """A few tokens of many adapters of high ranks, many of low ones."""
+    x, y, a, b, ids, scales = _case(11, T, K, N, E, r, dtype)
+    say("ranks", T, K, N, E, r, dtype)
+    dev = [t.cuda() for t in (x, a, b)]
+    plan = Q.lora_group(ids.cuda(), E)
+    yd = y.cuda()
+    out = Q.lora_add(yd, *dev, *plan, scales=scales.cuda())
+    _check(out, x, y, a, b, ids, scales)
+    assert torch.equal(out.cpu()[ids < 0], y[ids < 0])
+    assert torch.equal(Q.lora_add(yd, *dev, *plan, scales=scales.cuda(), out=yd), out)
+
+
+@pytest.mark.parametrize("T", [20, 200])
+@pytest.mark.parametrize("r", [24, 32, 40, 64, 72, 128])
+def test_nan_stays_in_its_row_and_column_whatever_the_rank(r, T):
+    """A NaN of x makes NaN of its token alone, an infinity of B of its column of its adapter alone, one of A of all of
+    its adapter's tokens and columns."""
+    x, y, a, b, _, _ = _case(12, T, 136, 200, 2, r, "bf16")
+    ids = (torch.arange(T) % 3 - 1).to(torch.int32)
+    plan = Q.lora_group(ids.cuda(), 2)
+
+    def bad(x, a, b):
+        return ~Q.lora_add(y.cuda(), x.cuda(), a.cuda(), b.cuda(), *plan).cpu().isfinite()
+    row, last = 4, 199     # (of adapter 0)
+    for place in ((0, 0), (135, r - 1)):
+        x1, a1, b1 = x.clone(), a.clone(), b.clone()
+        x1[row, place[0]] = float("nan")
+        want = torch.zeros(T, 200, dtype=torch.bool)
+        want[row] = True
+        assert torch.equal(bad(x1, a, b), want)
+        b1[0, last, place[1]] = float("inf")
+        want = torch.zeros(T, 200, dtype=torch.bool)
+        want[ids == 0, last] = True
+        assert torch.equal(bad(x, a, b1), want)
+        a1[1, place[1], place[0]] = float("nan")
+        want = (ids == 1).view(-1, 1).expand(T, 200)
+        assert torch.equal(bad(x, a1, b), want)
