@@ -326,3 +326,79 @@ def test_whole_items_in_any_order(seqs, heads):
     say("whole items", seqs, heads)
     Batch(40, lengths, [min(m, n) for m, n in zip(new, lengths)], heads, 1, 64, "f16").check()
     Batch(41, [70] * seqs, [1] * seqs, heads, 2, 64, "bf16").check(offsets=None)
+
+
+# 2048 columns of a sequence and more: the tiles of 256 columns (of 256 channels 128)
+LONG = [([700, 90], [300, 3], 1, 8, 128), ([2200], [260], 2, 8, 128), ([700, 90], [520, 3], 2, 4, 64), ([400, 0, 300], [210, 0, 129], 1, 16, 64),
+        ([500, 64], [260, 1], 1, 8, 256)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lengths,new,heads,group,D", LONG)
+def test_long_prompts(lengths, new, heads, group, D, dtype):
+    """Every mask, twice the same, with `most` known and not."""
+    say("long prompts", lengths, new, heads, group, D, dtype)
+    b = Batch(42, lengths, new, heads, group, D, dtype)
+    out = b.check()
+    assert torch.equal(b.run()[0], out)
+    b.check(most=None)
+    b.check(causal=False)
+    b.check(window=100, scale=-0.2)
+
+
+@pytest.mark.parametrize("window", [1, 31, 33, 63, 64, 65, 96, 127, 256, 300])
+@pytest.mark.parametrize("D", [64, 128])
+def test_window_edges_of_long_prompts(D, window):
+    say("window edges, long", D, window)
+    Batch(43, [500, 450], [270, 256], 1, 8, D, "bf16").check(window=window)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_nan_in_long_prompts(D, dtype):
+    """NaN values and infinite keys of a token, in the first and in the last block of channels: the rows that see it."""
+    say("NaN, long", D, dtype)
+    n, new, heads, group = 500, 260, 2, 8
+    b = Batch(44, [n, 100], [new, 1], heads, group, D, dtype)
+    for token, window, block in ((250, 0, 0), (499, 0, D // 32 - 1), (400, 70, 0), (320, 33, D // 32 - 1), (3, 0, 0)):
+        ref, _ = b.run(window=window)
+        k, v = (torch.zeros(1, heads, D, dtype=b.dtype) for _ in range(2))
+        v[0, 0, 32 * block + 1] = float("nan")
+        k[0, 1, 32 * block + 31] = float("inf")
+        slot = (b.table[0, token // 64] * 64 + token % 64).view(1).cuda()
+        kept = b.cache.clone()
+        Q.kv4_write(b.cache, k.cuda(), v.cuda(), slot)
+        out, _ = b.run(window=window)
+        b.cache.copy_(kept)
+        pos = torch.arange(n - new, n)
+        sees = (pos >= token) & (pos < token + window if window else pos >= 0)
+        sees = torch.cat([sees, torch.zeros(1, dtype=torch.bool)])
+        want = torch.zeros(out.shape, dtype=torch.bool)
+        want[sees, :group, 32 * block:32 * block + 32] = True     # the block of head 0
+        want[sees, group:] = True                                 # a NaN score of head 1
+        assert torch.equal(out.cpu().isnan(), want), (token, window, block)
+        assert torch.equal(out.cpu()[~sees], ref.cpu()[~sees])
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_pages_outside_the_cache_of_long_prompts(D):
+    b = Batch(45, [400, 300], [260, 256], 1, 8, D, "f16")
+    for page, bad in ((0, -1), (2, 1 << 24), (6, -(1 << 31)), (4, b.cache.shape[0])):
+        table = b.table.clone()
+        table[0, page] = bad
+        known = [torch.arange(n) // 64 != (page if i == 0 else -1) for i, n in enumerate(b.lengths)]
+        q, cache, _, lengths = b.args()
+        out = Q.kv4_attention(q, cache, table.cuda(), lengths, offsets=torch.tensor(b.offsets, dtype=torch.int32).cuda(), most=260)
+        want, _, tol = A.attention(b.q.double(), b.k, b.v, b.lengths, b.offsets, b.group, b.dtype, known=known)
+        assert bool(((out.cpu().double() - want).abs() <= tol).all()), (page, bad)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lengths,new,heads,group,D", [([70, 9, 300], [5, 5, 5], 2, 4, 128), ([100, 64, 65], [1, 64, 33], 1, 4, 128),
+                                                       ([500], [500], 2, 1, 64), ([200, 1, 130], [150, 1, 130], 1, 8, 128),
+                                                       ([333, 40], [77, 40], 1, 3, 256)])
+def test_without_most(lengths, new, heads, group, D, dtype):
+    """The form that is taken when the rows of all are what a sequence might have: to the same bound."""
+    b = Batch(46, lengths, new, heads, group, D, dtype)
+    b.check(most=None)
+    b.check(most=None, window=50)
