@@ -79,7 +79,7 @@ def rotary_frequencies(dim: int, base: float = 10000.0, scaling: str = "none", f
     * ``ramp``: pairs that turn more than ``high`` times over ``original`` keep
       their frequency, those that turn less than ``low`` times are divided by
       ``factor``, with a ramp over the pair's number between them; the attention
-      factor is 0.1 ln(factor) + 1;
+      factor is 0.1 ln(factor) + 1 (1 for factors up to 1);
     * ``bands``: the same with a ramp over the turns, and no attention factor."""
     if dim < 2 or dim % 2 or base <= 0 or factor <= 0:
         _fail(_q.QUICK_ERR_SHAPE, "rotary_frequencies: dim must be even and positive, base and factor positive (dim=%d)",
@@ -94,6 +94,8 @@ def rotary_frequencies(dim: int, base: float = 10000.0, scaling: str = "none", f
     elif scaling in ("ramp", "bands"):
         if original <= 0 or not 0 < low < high:
             _fail(_q.QUICK_ERR_INVALID_ARG, "rotary_frequencies: %s needs original > 0 and 0 < low < high", scaling)
+        if scaling == "ramp" and base <= 1:
+            _fail(_q.QUICK_ERR_INVALID_ARG, "rotary_frequencies: a ramp needs pairs that turn slower from one to the next")
 
         def pair(turns):
             # number of the pair that turns so often over `original`
