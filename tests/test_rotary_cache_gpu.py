@@ -202,3 +202,17 @@ def test_nothing_to_do():
     Q.kv4_write(cache, x, x, none)
     assert Q.kv4_read(cache, none)[0].shape == (0, 3, 64)
     assert Q.rotary(x, none, _freqs(8).cuda()).shape == (0, 3, 64)
+
+
+def test_rotary_angles_of_far_positions():
+    """Frequency 1, positions up to 2^31: cosine and sine themselves, against those of the whole number of radians.  The
+    turns are off by the roundings of 1 / (2 pi) (2^-53.8 of them) and of the product (2^-53), 2^-21.3 of a radian
+    together, the rest of a turn by 2^-26 of one in binary32 (2^-23.3), and the functions by two last places (2^-23)."""
+    g = A.gen(13)
+    pos = torch.cat([torch.randint(1 << 30, (1 << 31) - 1, (20000,), generator=g), torch.randint(-(1 << 31), 1 << 20, (20000,), generator=g),
+                     torch.tensor([(1 << 31) - 1, -(1 << 31)])])
+    x = torch.tensor([1.0, 0.0]).expand(pos.shape[0], 1, 2).contiguous()
+    y = Q.rotary(x.cuda(), pos.to(torch.int32).cuda(), torch.ones(1, dtype=torch.float64, device="cuda")).cpu().double()
+    angle = pos.double()
+    err = (y[:, 0] - torch.stack([torch.cos(angle), torch.sin(angle)], 1)).abs().max()
+    assert float(err) <= 2.0 ** -21.3 + 2.0 ** -23.3 + 2.0 ** -23, float(err)
