@@ -78,7 +78,8 @@ int quick_rotary(const void* x, int dtype, int64_t x_token, int64_t x_head, int6
  *   slots  int32 [T]; one outside 0 .. 64 * pages - 1 (a padded token's -1,
  *          say) is passed over.  Slots of a call have to differ: of two equal
  *          ones the slot keeps parts of either
- * Other slots keep their bytes.  T < 2^24.  T == 0 is a valid no-op.
+ * Other slots keep their bytes.  T < 2^24 and ceil(T / (2048 / D)) * heads < 2^24
+ * (SHAPE).  T == 0 is a valid no-op.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, HIP. */
 int quick_kv4_write(const void* k, const void* v, int dtype, int64_t k_token, int64_t k_head, int64_t v_token,
                     int64_t v_head, const int32_t* slots, int64_t T, int64_t heads, int64_t D, void* cache,
@@ -87,7 +88,7 @@ int quick_kv4_write(const void* k, const void* v, int dtype, int64_t k_token, in
 /* k, v [T][heads][D] of `dtype` (f16, bf16 or f32; 16-byte aligned) = the
  * values that slots[i] holds, rounded where the type cannot hold them (a scale
  * of 255 gives NaN); zero for a slot outside the cache.  Either may be NULL.
- * Errors as quick_kv4_write. */
+ * Limits and errors as quick_kv4_write. */
 int quick_kv4_read(const void* cache, int64_t pages, const int32_t* slots, int64_t T, int64_t heads, int64_t D,
                    int dtype, void* k, void* v, void* stream);
 

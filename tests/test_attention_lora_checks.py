@@ -308,3 +308,13 @@ def test_headers_compile_as_plain_c(tmp_path):
                     os.path.join(libdir, "libquick.so"), "-Wl,-rpath," + libdir], check=True)
     assert subprocess.run([exe]).returncode == 0
     assert (Q.KV4_PAGE, Q.LORA_MAX_RANK) == (64, 128)
+
+
+def test_abi_most_workgroups_of_the_cache():
+    """As many tokens and heads as the header says, and no more."""
+    L = Q.lib()
+    for d in (64, 128, 256):
+        t = (1 << 24) // 1024 * (2048 // d)        # one workgroup too many
+        assert L.quick_kv4_write(A, A, 0, 0, 0, 0, 0, A, t, 1024, d, A, 10, None) == SHAPE
+        assert L.quick_kv4_read(A, 10, A, t, 1024, d, 0, A, A, None) == SHAPE
+        assert L.quick_kv4_write(A, A, 0, 0, 0, 0, 0, A, t - 2048 // d + 1, 1024, d, A, 10, None) == SHAPE
