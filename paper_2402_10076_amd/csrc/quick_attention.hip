@@ -657,8 +657,10 @@ void launch_attention(const AttnArgs& a, int columns, hipStream_t hs)
     else {
         launch_tiled_attention(a, DT, D, columns, hs);
         const dim3 grid(a.workers, columns * D / 2048);
-        if (columns == 128) attn_join_kernel<DT, D, 128><<<grid, 256, 0, hs>>>(a);
-        else attn_join_kernel<DT, D, 256><<<grid, 256, 0, hs>>>(a);
+        if constexpr (D <= 128) {
+            if (columns == 256) return attn_join_kernel<DT, D, 256><<<grid, 256, 0, hs>>>(a);
+        }
+        attn_join_kernel<DT, D, 128><<<grid, 256, 0, hs>>>(a);
     }
 }
 template <int DT>
