@@ -612,15 +612,18 @@ int columns_of(const quick_attention_t& a)
 // that a second launch, and the plan before the first page, cost more than unequal
 // lengths do.  Of 8 cache heads of 128 read by 4 each, against shared out: 1
 // sequence of 1000 tokens 9.8 us and 13.9, of 3000 12.7 and 13.9, of 4000 15.9 and
-// 14.1; 64 of 1500 21.6 and 23.3, 256 of 100 to 3000 89 and 95.  Many items even
-// out when the longest begin first: 1024 of 37 to 4096 tokens 54.9 and 64.4; 8
-// sequences of 4091 among 128 of 60 22.3 and 24.4.  32 columns of 256 channels
-// leave a unit four waves: 16 of 100 to 3000 38 and 34.
+// 14.1; 64 of 1500 21.6 and 23.3.  Items that do not all begin at once even out
+// when the longest begin first: of 49 to 64 pages 560 items 34.7 and 37.9 (lengths
+// of 37 to 4096) or 60.9 and 61.2 (of 3200 to 4096), 960 of them 53.3 and 61.9, or
+// 95.9 and 96.4 (700 of 140 sequences, more than are put in order, 51.2 and 48.9,
+// or 68.4 and 75.2); 64 of them 17.6 and 13.7, or 17.6 and 17.2; 384 28.7 and 26.9,
+// or 43.3 and 44.9 (of 256 channels 58.2 and 53.5, or 82.1 and 81.3).  32 columns
+// of 256 channels leave a unit four waves: 16 of 100 to 3000 38 and 34.
 bool whole_items(const quick_attention_t& a)
 {
     const int64_t n = columns_most(a), items = a.seqs * a.heads;
     if (n > 32) return false;
-    return a.table_width <= (n > 16 && a.D > 128 ? 16 : items < 1024 ? 48 : kWholePages);
+    return a.table_width <= (n > 16 && a.D > 128 ? 16 : items <= 2 * kUnits ? 48 : kWholePages);
 }
 
 int workers_of(const quick_attention_t& a)

@@ -402,3 +402,15 @@ def test_without_most(lengths, new, heads, group, D, dtype):
     b = Batch(46, lengths, new, heads, group, D, dtype)
     b.check(most=None)
     b.check(most=None, window=50)
+
+
+@pytest.mark.parametrize("seqs,heads", [(64, 8), (65, 8), (171, 3)])
+def test_tables_of_64_pages(seqs, heads):
+    """Where items of 49 to 64 pages begin to be taken whole: a long sequence among short ones, some without a query."""
+    g = A.gen(47, seqs)
+    lengths = [int(n) for n in torch.randint(0, 200, (seqs,), generator=g)]
+    lengths[5] = 64 * 64 - 3
+    new = [int(n) % 3 for n in range(seqs)]
+    say("64 pages", seqs, heads)
+    Batch(48, lengths, [min(m, n) for m, n in zip(new, lengths)], heads, 1, 64, "bf16", width=64).check()
+    Batch(49, lengths, [1] * seqs, heads, 1, 64, "f16", width=64).check(window=700, offsets=None)
