@@ -597,15 +597,19 @@ int64_t columns_most(const quick_attention_t& a) { return std::min(a.most, a.T) 
 // Up to 128 the stream kernel, in tiles of 32 (16 sequences of 2000 to 8000
 // tokens, 8 cache heads of 128: n = 40 43 us, 64 44, 96 57, 128 71; the tiled
 // one, half of whose waves the first of these leave idle, 57, 60, 65, 72; of 256
-// channels n = 80 124 and 162).  Of the tiled forms 256 columns with many
-// queries: 7 % faster there (8192 queries of 8 heads each: 1109 us, 1194 with
-// 128), and as much slower with few (1 to 501 of 4 heads of 64, a window: 84 us,
-// 76 with 128); its registers do not suffice for 256 channels.
+// channels n = 80 124 and 162).  Of the tiled forms 256 columns with many queries
+// of 128 channels: 8 sequences of 4000, 8 cache heads, n = 2056 311 us, 323 with
+// 128; 4096 531 and 570; 16384 (two sequences) 429 and 461.  With fewer the columns
+// that its last tile has not cost as much as that gains: n = 1296 216 and 215, 1040
+// 178 and 181, 520 115 and 110; 1 to 256 queries, n = 1024 at most, 112 and 108.  Of
+// 64 channels, where the vector instructions bound both, 128 is the faster one
+// throughout (n = 2048 200 and 193 us, 16384 304 and 299), and of 256 the
+// registers do not suffice.
 int columns_of(const quick_attention_t& a)
 {
     const int64_t n = columns_most(a);
     if (n <= 128) return n <= 16 ? 16 : 32;
-    return n < 2048 || a.D > 128 ? 128 : 256;
+    return n >= 2048 && a.D == 128 ? 256 : 128;
 }
 
 // Whether a workgroup takes an item each: one tile of a sequence, of so few pages
@@ -660,7 +664,7 @@ void launch_attention(const AttnArgs& a, int columns, hipStream_t hs)
     else {
         launch_tiled_attention(a, DT, D, columns, hs);
         const dim3 grid(a.workers, columns * D / 2048);
-        if constexpr (D <= 128) {
+        if constexpr (D == 128) {
             if (columns == 256) return attn_join_kernel<DT, D, 256><<<grid, 256, 0, hs>>>(a);
         }
         attn_join_kernel<DT, D, 128><<<grid, 256, 0, hs>>>(a);

@@ -141,7 +141,6 @@ struct Unstage {
             }
             if constexpr (STEP >= 2) {
                 u4_t lo, hi;
-                // (D == 64: with eight waves both of a pair write the same)
                 const int tile = D == 64 ? y : 4 * h + (S::SHARE == 1 ? 2 * y + STEP - 2 : 2 * y + part);
                 if constexpr (STEP == 2 || (D > 64 && S::SHARE == 1)) {
                     value_words<DT, S::VW, STEP - 2>(a[h], b[h], sa[h], sb[h], lo, hi);
@@ -484,7 +483,7 @@ __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(At
 template <int DT, int D>
 void launch(const AttnArgs& a, int columns, hipStream_t hs)
 {
-    if constexpr (D <= 128) {
+    if constexpr (D == 128) {
         if (columns == 256) return attn_tiled_kernel<DT, D, 8, 3><<<a.workers, 512, 0, hs>>>(a);
     }
     attn_tiled_kernel<DT, D, 4, D == 64 ? 3 : 2><<<a.workers, 256, 0, hs>>>(a);
