@@ -135,6 +135,8 @@ typedef struct quick_attention {
  * `dtype`, the result once more.  Deterministic.
  * workspace: 16-byte aligned, of quick_kv4_attention_workspace_bytes() (0: may
  * be NULL); calls that share one must be ordered.
+ * `most` chooses the kernels for all sequences of a call: prompts beside many
+ * single tokens are faster as two calls, of their rows each.
  * T < 2^24, q_heads / heads <= 64, seqs <= QUICK_KV4_MAX_SEQS, table_width <
  * 2^24, T * q_heads * D < 2^40, most >= 1, window >= 0 and without `causal` 0
  * (SHAPE).  T == 0 or seqs == 0 is a valid no-op.

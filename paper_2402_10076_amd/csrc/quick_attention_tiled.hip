@@ -187,7 +187,10 @@ __device__ void spoil(f16_t (&o)[D / 32], const uint8_t* page, int lo, int hi, i
 // Bound by both: of 128 channels a page is 1024 cycles of matrix instructions for
 // a wave and some 1250 of vector ones (32 exponentials a lane among them), which overlap
 // in part: 8192 queries of 64 heads 1110 us, 990 TFLOP/s, matrix instructions
-// busy 45 % of the cycles.  Of 64 channels it is 512 and 1100: the vector ones.
+// busy 45 % of the cycles.  Of 64 channels it is 512 and 1100: the vector ones.  Of
+// 256 a wave's sums and queries fill one register file, and moves between the two
+// are a third to a half of the vector instructions: 2 sequences of 4096 tokens,
+// the last 2048 as queries, 32 heads on 8, 662 us, 620 TFLOP/s.
 template <int DT, int D, int NW, int NB>
 __global__ __launch_bounds__(64 * NW, D > 128 ? 1 : 2) void attn_tiled_kernel(AttnArgs a)
 {

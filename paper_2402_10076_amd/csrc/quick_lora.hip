@@ -441,7 +441,11 @@ int64_t tiles_of(int64_t R, int64_t E)
 // Slices of the channels: a workgroup for each compute unit and some more, whole
 // rounds of its waves (64 channels each with 64 rows, 128 with 16), and 16 at
 // most, as the second product adds them up (512 tokens, 5120 channels: 27.2 us,
-// 29.2 with eight).
+// 29.2 with eight).  What it counts are the most tiles there can be, and with 64
+// rows LDS holds one workgroup a unit, so that a few more than the units run a
+// round of their own: 4096 tokens, 5120 channels to 15360, rank 64, of four
+// adapters with 1024 each, 64 tiles of 4 slices, take 83 us, of five with 819, 65
+// tiles, 104.
 void slices_of(int64_t R, int64_t K, int64_t E, int32_t* slices, int32_t* slice)
 {
     const int64_t round = tile_rows(R, E) == 64 ? 512 : 1024, rounds = ceil_div(K, round);

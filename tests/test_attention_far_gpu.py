@@ -185,3 +185,41 @@ def test_blocks_beyond_the_type(dtype, form):
     held = cache.clone()
     held[token // 64, 0, value] = least - 1
     assert run(held).isfinite().all()
+
+
+@pytest.mark.parametrize("form", [FORMS[1], FORMS[5], FORMS[9], FORMS[12]], ids=lambda f: "-".join(map(str, f[:3])))
+def test_replayed_with_near_and_far_scores(form):
+    """A captured call, replayed with queries whose scores are near, far and near again: the bits of eager calls."""
+    D, heads, group, lengths, new, width = form
+    say("replayed", form)
+    g = A.gen(54, D, heads)
+    need = [-(-n // 64) for n in lengths]
+    table = torch.zeros((len(lengths), width or max(need)), dtype=torch.int32)
+    cache, at, offsets = Q.kv4_cache(sum(need), heads, D), 0, [0]
+    for b, n in enumerate(lengths):
+        table[b, :need[b]] = torch.arange(at, at + need[b])
+        Q.kv4_write(cache, *(A.normal(g, n, heads, D).cuda() for _ in "kv"), torch.arange(at * 64, at * 64 + n, dtype=torch.int32).cuda())
+        at += need[b]
+        offsets.append(offsets[-1] + new[b])
+    q = A.normal(g, offsets[-1], heads * group, D, scale=1.5).cuda()
+    far = q.clone()
+    far[::2, ::3] *= 8192.0
+    table, ln, off = table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), torch.tensor(offsets, dtype=torch.int32).cuda()
+    at = q.clone()
+
+    def run():
+        return Q.kv4_attention(at, cache, table, ln, offsets=off, most=max(new), scale=1e3)
+    want = {}
+    for name, x in (("near", q * 1e-3), ("far", far)):
+        at.copy_(x)
+        want[name] = run()
+    assert want["far"].isfinite().all() and not torch.equal(want["near"], want["far"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for name, x in (("near", q * 1e-3), ("far", far), ("near", q * 1e-3), ("far", far), ("near", q * 1e-3)):
+        at.copy_(x)
+        out.fill_(7)
+        graph.replay()
+        assert torch.equal(out, want[name]), name
+        assert torch.equal(run(), want[name]), name
