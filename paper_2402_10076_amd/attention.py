@@ -302,8 +302,9 @@ def kv4_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, len
 
     A row that sees nothing is zero; rows of no sequence are left as they
     were (in a new result: undefined).  lse: f32 [T][q_heads], filled with the
-    logarithm of the softmax's sum.  workspace: a tensor of kv4_attention_workspace_bytes(); one is taken
-    from torch's allocator if none is given."""
+    logarithm of the softmax's sum.  workspace: a tensor of
+    kv4_attention_workspace_bytes(); one is taken from torch's allocator if
+    none is given."""
     what = "kv4_attention"
     sizes = _usual(q, cache, table, lengths, offsets)
     if sizes is None:
